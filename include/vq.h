@@ -330,6 +330,172 @@ vq_status vq_gemm_small_batch_normalized(const vq_format* fmt, const void* d_idx
                                          const void* d_norm_codes, const void* d_norm_lut, int norm_block_cols, const void* d_X,
                                          void* d_Y, int batch, void* stream);
 
+/* ---- between the linear layers of a decode step ----------------------------------------------------------------
+ * The paper's decode step (Sec. 1: per generated token every weight is read once; Sec. 3.2) is a transformer block's:
+ * between the q/k/v projections and the output projection sit the rotation of queries and keys, the cache of keys and
+ * values and the attention that reads it, and between blocks the residual stream and its norms.  The entry points
+ * below are those, on the activations (binary16) that the products above write and read.  Layouts are this
+ * library's.  They are ordered behind everything that `stream` holds: what they read may be written by any
+ * earlier work of the stream.  They launch on the current device, and all their pointers are that device's.
+ *
+ * Cache: a pool of pages per layer, page_tokens tokens each.
+ *   keys, values : [n_pages][n_kv_heads][page_tokens][head_dim], binary16 (VQ_KV_FP16) or signed 8-bit (VQ_KV_INT8);
+ *   their scales : VQ_KV_INT8 only, binary32 [n_pages][n_kv_heads][page_tokens], >= 0: value = scale * integer.
+ *   table        : int32 [n_seqs][table_stride]: the pages of each sequence in order; token t of sequence s is token
+ *                  t mod page_tokens of page table[s][t / page_tokens].
+ *   len          : int32 [n_seqs], tokens that a sequence has in the cache.  The kernels take it between 0 and
+ *                  table_stride * page_tokens, whatever is stored.  A page number outside 0..n_pages-1 in the table
+ *                  is never followed: its tokens are neither read (vq_kv_attention leaves them out, as if masked)
+ *                  nor written.
+ *   refs         : int32 [n_pages], how many table rows hold a page; 0 = free.
+ * Pages that two sequences share (vq_kv_fork) are full, so appending never writes to a shared page. */
+typedef enum { VQ_KV_FP16 = 0, VQ_KV_INT8 = 1 } vq_kv_type;
+
+typedef struct {
+  int32_t n_pages;      /* pages of one layer's pool                                    */
+  int32_t page_tokens;  /* tokens per page: 8, 16, 32, 64, 128 or 256                   */
+  int32_t n_kv_heads;   /* key/value heads                                              */
+  int32_t head_dim;     /* a multiple of 16, up to 256 (vq_kv_attention: 64, 80, 96, 128, 192, 256) */
+  int32_t kv_type;      /* vq_kv_type                                                   */
+} vq_kv_format;
+
+/* One layer's pool (device pointers).  Scales NULL iff kv_type == VQ_KV_FP16. */
+typedef struct {
+  void* d_k;
+  void* d_v;
+  void* d_k_scale;
+  void* d_v_scale;
+} vq_kv_pool;
+
+/* Table and lengths (device pointers, 4-byte aligned), the same for every layer. */
+typedef struct {
+  void* d_table;         /* int32 [n_seqs][table_stride]                                */
+  void* d_len;           /* int32 [n_seqs]                                              */
+  int32_t n_seqs;        /* 1..65536                                                    */
+  int32_t table_stride;  /* pages a row has room for; table_stride * page_tokens <= 2^30 */
+} vq_kv_seqs;
+
+typedef struct {
+  size_t pool_bytes;     /* keys of one layer (values: as many)                         */
+  size_t scale_bytes;    /* scales of one layer's keys (values: as many); 0 for FP16    */
+  size_t page_bytes;     /* keys, values and scales of one page of one layer            */
+} vq_kv_info_t;
+
+/* Sizes of a cache.  Host only.  Errors: NULL, FORMAT (kv_type, page_tokens, head_dim), SHAPE (counts <= 0). */
+vq_status vq_kv_info(const vq_kv_format* fmt, vq_kv_info_t* out);
+
+/* Attention of one new token per sequence over the cache:
+ *   out[s][h] = sum_t softmax_t(scale * q[s][h] . k[s][t][h / (n_q_heads / n_kv_heads)]) v[s][t][...],
+ * t over the sequence's last `window` tokens (window 0: over all len[s] of them; the new token's own key and value are
+ * in the cache, vq_kv_append put them there).
+ *   n_q_heads : a multiple of n_kv_heads (any group size).
+ *   d_q       : device binary16, row s at d_q + s * q_stride elements, heads one after the other (q_stride a
+ *               multiple of 8, at least n_q_heads * head_dim).
+ *   d_out     : device binary16, rows out_stride elements apart (as q_stride).  A sequence without tokens gets zeros.
+ *   d_lse     : device binary32 [n_seqs][n_q_heads], log of the softmax's denominator (natural, of scale * q . k),
+ *               -inf for a sequence without tokens; or NULL.  4-byte aligned.
+ *   d_ws      : at least vq_kv_attention_workspace_bytes(fmt) bytes, 16-byte aligned.  Rules as WORKSPACE above, for
+ *               calls of this entry point: zero-filled once, then free for calls of any format, batch and length.
+ *               Not to be shared with the products' workspace.
+ * Scores, softmax and sums are binary32; one rounding to binary16 at the end.  Masked places and what lies behind a
+ * sequence's last token are not read as numbers: an infinity or NaN there changes nothing.
+ * Errors: NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (head_dim), CUDA. */
+size_t vq_kv_attention_workspace_bytes(const vq_kv_format* fmt);
+vq_status vq_kv_attention(const vq_kv_format* fmt, const vq_kv_pool* pool, const vq_kv_seqs* seqs, int n_q_heads, const void* d_q,
+                          int64_t q_stride, void* d_out, int64_t out_stride, void* d_lse, float scale, int window, void* d_ws,
+                          size_t ws_bytes, void* stream);
+
+/* Rotary position embedding of vq_kv_append: the pair (a, b) of a query or key at position t becomes
+ * (a cos - b sin, b cos + a sin) with the table's cosine and sine of position t and the pair's number. */
+typedef struct {
+  const void* d_cos_sin;   /* binary32 [n_positions][rot_dim / 2][2]: cosine, sine (16-byte aligned)           */
+  int32_t n_positions;     /* at least table_stride * page_tokens: every position a sequence can have         */
+  int32_t rot_dim;         /* leading dimensions that are rotated: a multiple of 16, at most head_dim         */
+  int32_t interleaved;     /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1)                          */
+  int32_t n_q_heads;       /* heads of d_q; 0 with d_q == NULL: keys only                                     */
+  const void* d_q;         /* binary16 [n_tokens] rows, q_stride elements apart                               */
+  void* d_q_out;           /* rotated queries, rows q_out_stride elements apart; may be d_q itself (same stride) */
+  int64_t q_stride, q_out_stride;
+} vq_kv_rotary;
+
+/* New tokens into the cache: the keys rotated (rotary != NULL), keys and values written to the pages that the table
+ * names, the tokens' queries rotated.
+ *   d_len    : lengths WITH the new tokens (vq_kv_reserve has counted them and given them pages).
+ *   d_starts : device int32 [n_seqs + 1], never falling: rows starts[s]..starts[s+1]-1 are the new tokens of sequence
+ *              s, its last ones in the cache; rows from starts[n_seqs] on are nobody's: neither they nor their
+ *              places in d_q_out are touched.  NULL: one token per sequence, row s for sequence s (n_tokens == n_seqs;
+ *              a sequence of length 0 takes none).
+ *   d_k, d_v : device binary16 [n_tokens] rows of n_kv_heads * head_dim, k_stride / v_stride elements apart.
+ * Rotation is binary32, rounded once.  VQ_KV_INT8 stores, per token and head, scale = max|x| / 127 and the integers
+ * nearest x / scale (ties to even) of the rotated, not yet rounded x; a row of zeros has scale 0; one that holds
+ * an infinity or NaN reads back as no number.  Strides: multiples of 8.
+ * Errors: NULL, FORMAT, SHAPE, ALIGN, CUDA. */
+vq_status vq_kv_append(const vq_kv_format* fmt, const vq_kv_pool* pool, const vq_kv_seqs* seqs, const void* d_starts, int n_tokens,
+                       const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride, const vq_kv_rotary* rotary, void* stream);
+
+/* The cache's books: table, lengths and reference counts are kept on the device, so that these calls can stand in a
+ * captured decode step.  Pages are given out lowest number first, in the order of the sequences or of the list, so equal
+ * books give equal books.  d_refs, lists and statuses are int32, 4-byte aligned; d_ws: at least
+ * vq_kv_pages_workspace_bytes(fmt, n_seqs) bytes, 16-byte aligned, contents ignored; calls that may overlap need
+ * different ones.  Table entries behind a sequence's last page are left as they were.
+ *
+ * vq_kv_reserve: sequence s grows by d_new[s] tokens (int32 [n_seqs], negative counts as 0; NULL: by one each): the
+ *   pages that it needs for them are taken and entered in its row, len[s] grows.  d_status[0] = pages that were
+ *   missing, d_status[1] = sequences whose row is too short (pages are not counted then); if either is not 0 the call
+ *   has changed nothing else.
+ * vq_kv_fork: entry i of d_pairs (int32 [n_pairs][2]) makes sequence d_pairs[i][1] a continuation of sequence
+ *   d_pairs[i][0]: it shares the parent's full pages, and the tokens of a last page that is not full are copied to a
+ *   page of its own in every layer.  All parents are read as they were before the call.  An entry is left out
+ *   (d_status[1] counts them) if a number is no sequence's, the child is not empty (len 0), or an earlier entry has
+ *   the same child.  d_status[0] = pages missing; if not 0 the call has changed nothing else.  n_pairs 1..1024.
+ * vq_kv_free: the listed sequences (int32 [n_slots], 1..65536; numbers that are no sequence's and repeated ones do
+ *   nothing) give their pages back and are empty.
+ * vq_kv_compact: the pages in use move to the lowest numbers, in every layer: those at or above the count of used
+ *   pages, in ascending order, go to the free ones below it, in ascending order.  Table rows and counts follow.
+ *   d_status[0] = pages in use, d_status[1] = pages moved.
+ * vq_kv_copy_pages: page d_pairs[i][0] to page d_pairs[i][1] (int32 [n_pairs][2]) in every layer, no books.  Pairs that
+ *   name no page are left out.  No page may be the destination of two pairs, or destination and source.
+ *   n_pairs 1..2^24.
+ *   pools : HOST array of n_layers (1..VQ_KV_MAX_LAYERS) pools.
+ * Errors: NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, CUDA. */
+#define VQ_KV_MAX_LAYERS 120
+size_t vq_kv_pages_workspace_bytes(const vq_kv_format* fmt, int n_seqs);
+vq_status vq_kv_reserve(const vq_kv_format* fmt, const vq_kv_seqs* seqs, void* d_refs, const void* d_new, void* d_status, void* d_ws,
+                        size_t ws_bytes, void* stream);
+vq_status vq_kv_fork(const vq_kv_format* fmt, const vq_kv_pool* pools, int n_layers, const vq_kv_seqs* seqs, void* d_refs,
+                     const void* d_pairs, int n_pairs, void* d_status, void* d_ws, size_t ws_bytes, void* stream);
+vq_status vq_kv_free(const vq_kv_format* fmt, const vq_kv_seqs* seqs, void* d_refs, const void* d_slots, int n_slots, void* stream);
+vq_status vq_kv_compact(const vq_kv_format* fmt, const vq_kv_pool* pools, int n_layers, const vq_kv_seqs* seqs, void* d_refs,
+                        void* d_status, void* d_ws, size_t ws_bytes, void* stream);
+vq_status vq_kv_copy_pages(const vq_kv_format* fmt, const vq_kv_pool* pools, int n_layers, const void* d_pairs, int n_pairs,
+                           void* stream);
+
+/* The residual stream between two blocks:  x' = x + residual_scale * gate * post(y),  h = pre(x'),
+ * with y a block's output (the product of its last projection), post and pre norms over a row's n_cols values:
+ *   VQ_NORM_RMS  : u * rsqrt(mean(u^2) + eps) * weight [+ bias]
+ *   VQ_NORM_LAYER: the same of u - mean(u).
+ * d_y NULL: x' = x.  d_post_w NULL: post(y) = y.  Biases may be NULL.  d_gate: binary16, one value per channel
+ * (VQ_GATE_CHANNEL) or per element (VQ_GATE_ELEMENT, rows gate_stride apart), NULL for VQ_GATE_NONE.
+ *   d_x, d_x_out : device, binary16 or binary32 (residual_type), rows x_stride / x_out_stride elements apart; d_x_out may
+ *                  be d_x (same stride) or NULL (x' is not stored).
+ *   d_h          : device binary16, or NULL with d_pre_w NULL (no norm behind).  It may be d_y (same stride).
+ * h is formed of x' before x' is rounded; everything is binary32 with one rounding per output.  n_cols up to 32768, any
+ * number; rows of whole 16-byte pieces (n_cols and strides multiples of 8) are read and written in those.
+ * Errors: NULL, FORMAT (kind, residual_type, gate), SHAPE, ALIGN, CUDA. */
+typedef enum { VQ_NORM_RMS = 0, VQ_NORM_LAYER = 1 } vq_norm_kind;
+typedef enum { VQ_RESIDUAL_FP16 = 0, VQ_RESIDUAL_FP32 = 1 } vq_residual_type;
+typedef enum { VQ_GATE_NONE = 0, VQ_GATE_CHANNEL = 1, VQ_GATE_ELEMENT = 2 } vq_gate_kind;
+typedef struct {
+  int32_t n_rows, n_cols;
+  int32_t kind;           /* vq_norm_kind, of both norms */
+  int32_t residual_type;  /* vq_residual_type            */
+  int32_t gate;           /* vq_gate_kind                */
+  float eps, residual_scale;
+  int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride;   /* elements; those of absent operands are ignored */
+} vq_norm_block;
+vq_status vq_residual_norm(const vq_norm_block* desc, const void* d_x, const void* d_y, const void* d_gate, const void* d_post_w,
+                           const void* d_post_b, const void* d_pre_w, const void* d_pre_b, void* d_x_out, void* d_h, void* stream);
+
 /* Uniformly quantized weights expanded to binary16: the yard-sticks of the transfer + decode
  * experiment (paper App. B: time to move and unpack a layer stored as FP16, INT8, INT4 or VQ),
  * timed beside vq_decode_weights.  w = s * q (Sec. 2.1), exact product rounded once to binary16.

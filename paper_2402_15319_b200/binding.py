@@ -7,6 +7,7 @@ import ctypes
 import functools
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 VQ_CB_FP16, VQ_CB_INT8_SCALED, VQ_CB_INT4_G128 = 0, 1, 2
 VQ_IMPL_AUTO, VQ_IMPL_GENERIC, VQ_IMPL_TUNED, VQ_IMPL_STREAM, VQ_IMPL_TILE = 0, 1, 2, 3, 4
@@ -102,6 +103,20 @@ _SIGNATURES = {
                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "vq_probe_read": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p]),
     "vq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
+    "vq_kv_info": (ctypes.c_int, [ctypes.c_void_p] * 2),
+    "vq_kv_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.c_void_p]),
+    "vq_kv_attention": (ctypes.c_int, [ctypes.c_void_p] * 3 + [ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                       ctypes.c_void_p, ctypes.c_float, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "vq_kv_append": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                    ctypes.c_void_p, ctypes.c_void_p]),
+    "vq_kv_pages_workspace_bytes": (ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_int]),
+    "vq_kv_reserve": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_size_t, ctypes.c_void_p]),
+    "vq_kv_fork": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int] + [ctypes.c_void_p] * 3 + [ctypes.c_int] + [ctypes.c_void_p] * 2 +
+                   [ctypes.c_size_t, ctypes.c_void_p]),
+    "vq_kv_free": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int, ctypes.c_void_p]),
+    "vq_kv_compact": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int] + [ctypes.c_void_p] * 4 + [ctypes.c_size_t, ctypes.c_void_p]),
+    "vq_kv_copy_pages": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]),
+    "vq_residual_norm": (ctypes.c_int, [ctypes.c_void_p] * 11),
 }
 
 
@@ -331,3 +346,228 @@ def vq_assign_indices(fmt: "VQFormat", d_W, d_cb, d_scale, d_hdiag, d_idx, strea
     _check(load().vq_assign_indices(ctypes.byref(c), _ptr(d_W), _ptr(d_cb), _ptr(d_scale), _ptr(d_hdiag), _ptr(d_idx),
                                     _stream(stream)), "vq_assign_indices")
 
+
+
+# ---- the cache, its attention, the residual stream ------------------------------------------------------------------
+
+VQ_KV_FP16, VQ_KV_INT8 = 0, 1
+VQ_KV_MAX_LAYERS = 120
+VQ_NORM_RMS, VQ_NORM_LAYER = 0, 1
+VQ_RESIDUAL_FP16, VQ_RESIDUAL_FP32 = 0, 1
+VQ_GATE_NONE, VQ_GATE_CHANNEL, VQ_GATE_ELEMENT = 0, 1, 2
+
+
+class _CKVFormat(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "n_kv_heads", "head_dim", "kv_type")]
+
+
+class _CKVPool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_k", "d_v", "d_k_scale", "d_v_scale")]
+
+
+class _CKVSeqs(ctypes.Structure):
+    _fields_ = [("d_table", ctypes.c_void_p), ("d_len", ctypes.c_void_p), ("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32)]
+
+
+class _CKVInfo(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_size_t) for n in ("pool_bytes", "scale_bytes", "page_bytes")]
+
+
+class _CKVRotary(ctypes.Structure):
+    _fields_ = [("d_cos_sin", ctypes.c_void_p), ("n_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("d_q", ctypes.c_void_p), ("d_q_out", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64)]
+
+
+class _CNormBlock(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("n_rows", "n_cols", "kind", "residual_type", "gate")] +
+                [("eps", ctypes.c_float), ("residual_scale", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("x_stride", "y_stride", "gate_stride", "x_out_stride", "h_stride")])
+
+
+@dataclass(frozen=True)
+class VQKVFormat:
+    n_pages: int
+    page_tokens: int
+    n_kv_heads: int
+    head_dim: int
+    kv_type: int
+
+    def c(self) -> _CKVFormat:
+        return _c_kv_format(self)
+
+
+@functools.lru_cache(maxsize=4096)
+def _c_kv_format(f: "VQKVFormat") -> _CKVFormat:
+    return _CKVFormat(f.n_pages, f.page_tokens, f.n_kv_heads, f.head_dim, f.kv_type)
+
+
+@dataclass(frozen=True)
+class KVInfo:
+    pool_bytes: int
+    scale_bytes: int
+    page_bytes: int
+
+
+class KVPool(NamedTuple):
+    """One layer's pool: keys and values, and their scales for VQ_KV_INT8."""
+    k: object
+    v: object
+    k_scale: object = None
+    v_scale: object = None
+
+
+class KVSeqs(NamedTuple):
+    """Page table (int32, a row per sequence) and lengths (int32)."""
+    table: object
+    length: object
+
+
+class KVRotary(NamedTuple):
+    """Cosines and sines, and the new tokens' queries (None: keys only)."""
+    d_cos_sin: object
+    n_positions: int
+    rot_dim: int
+    interleaved: int
+    n_q_heads: int = 0
+    d_q: object = None
+    q_stride: int = 0
+    d_q_out: object = None
+    q_out_stride: int = 0
+
+
+@dataclass(frozen=True)
+class VQNorm:
+    n_rows: int
+    n_cols: int
+    kind: int
+    residual_type: int
+    gate: int
+    eps: float
+    residual_scale: float
+    x_stride: int
+    y_stride: int = 0
+    gate_stride: int = 0
+    x_out_stride: int = 0
+    h_stride: int = 0
+
+    def c(self) -> _CNormBlock:
+        return _c_norm(self)
+
+
+@functools.lru_cache(maxsize=4096)
+def _c_norm(n: "VQNorm") -> _CNormBlock:
+    return _CNormBlock(n.n_rows, n.n_cols, n.kind, n.residual_type, n.gate, n.eps, n.residual_scale, n.x_stride, n.y_stride, n.gate_stride,
+                       n.x_out_stride, n.h_stride)
+
+
+_current_device = None
+
+
+def _here(*tensors) -> None:
+    """The calls below launch on the current device: a tensor of another one (or of the host) is refused."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = torch.cuda.current_device if torch.cuda.is_available() else lambda: 0
+    dev = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
+
+
+def _c_pool(pool: KVPool) -> _CKVPool:
+    _here(*pool)
+    return _CKVPool(*[_ptr(t) for t in pool])
+
+
+def _c_pools(pools):
+    return (_CKVPool * len(pools))(*[_c_pool(p) for p in pools])
+
+
+def _c_seqs(seqs: KVSeqs) -> _CKVSeqs:
+    table, length = seqs
+    _here(table, length)
+    if table.dim() != 2 or not table.is_contiguous() or length.dim() != 1 or not length.is_contiguous() or length.shape[0] != table.shape[0]:
+        raise ValueError("KVSeqs: a contiguous table, and a length for each of its rows")
+    return _CKVSeqs(table.data_ptr(), length.data_ptr(), table.shape[0], table.shape[1])
+
+
+def _bytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def vq_kv_info(fmt: VQKVFormat) -> KVInfo:
+    out = _CKVInfo()
+    _check(load().vq_kv_info(ctypes.byref(fmt.c()), ctypes.byref(out)), "vq_kv_info")
+    return KVInfo(int(out.pool_bytes), int(out.scale_bytes), int(out.page_bytes))
+
+
+def vq_kv_attention_workspace_bytes(fmt: VQKVFormat) -> int:
+    return load().vq_kv_attention_workspace_bytes(ctypes.byref(fmt.c()))
+
+
+def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int, d_q, q_stride: int, d_out, out_stride: int, d_lse, scale: float,
+                    window: int, d_ws, stream=None) -> None:
+    """One new token per sequence over the paged cache; window 0: all of it.  d_lse may be None."""
+    _here(d_q, d_out, d_lse, d_ws)
+    _check(load().vq_kv_attention(ctypes.byref(fmt.c()), ctypes.byref(_c_pool(pool)), ctypes.byref(_c_seqs(seqs)), int(n_q_heads), _ptr(d_q),
+                                  int(q_stride), _ptr(d_out), int(out_stride), _ptr(d_lse), float(scale), int(window), _ptr(d_ws), _bytes(d_ws),
+                                  _stream(stream)), "vq_kv_attention")
+
+
+def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens: int, d_k, k_stride: int, d_v, v_stride: int,
+                 rotary: KVRotary | None = None, stream=None) -> None:
+    """New tokens into the cache.  d_starts None: one token per sequence."""
+    _here(d_starts, d_k, d_v)
+    r = None
+    if rotary is not None:
+        _here(rotary.d_cos_sin, rotary.d_q, rotary.d_q_out)
+        r = ctypes.byref(_CKVRotary(_ptr(rotary.d_cos_sin), int(rotary.n_positions), int(rotary.rot_dim), int(rotary.interleaved),
+                                    int(rotary.n_q_heads), _ptr(rotary.d_q), _ptr(rotary.d_q_out), int(rotary.q_stride), int(rotary.q_out_stride)))
+    _check(load().vq_kv_append(ctypes.byref(fmt.c()), ctypes.byref(_c_pool(pool)), ctypes.byref(_c_seqs(seqs)), _ptr(d_starts), int(n_tokens),
+                               _ptr(d_k), int(k_stride), _ptr(d_v), int(v_stride), r, _stream(stream)), "vq_kv_append")
+
+
+def vq_kv_pages_workspace_bytes(fmt: VQKVFormat, n_seqs: int) -> int:
+    return load().vq_kv_pages_workspace_bytes(ctypes.byref(fmt.c()), int(n_seqs))
+
+
+def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, stream=None) -> None:
+    """Room for d_new tokens per sequence (None: one each); d_status: pages missing, sequences too long."""
+    _here(d_refs, d_new, d_status, d_ws)
+    _check(load().vq_kv_reserve(ctypes.byref(fmt.c()), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_new), _ptr(d_status), _ptr(d_ws),
+                                _bytes(d_ws), _stream(stream)), "vq_kv_reserve")
+
+
+def vq_kv_fork(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_pairs, n_pairs: int, d_status, d_ws, stream=None) -> None:
+    """pools: one KVPool per layer.  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
+    _here(d_refs, d_pairs, d_status, d_ws)
+    _check(load().vq_kv_fork(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_pairs),
+                             int(n_pairs), _ptr(d_status), _ptr(d_ws), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
+
+
+def vq_kv_free(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_slots, n_slots: int, stream=None) -> None:
+    _here(d_refs, d_slots)
+    _check(load().vq_kv_free(ctypes.byref(fmt.c()), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_slots), int(n_slots), _stream(stream)),
+           "vq_kv_free")
+
+
+def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, stream=None) -> None:
+    """d_status: pages in use, pages moved."""
+    _here(d_refs, d_status, d_ws)
+    _check(load().vq_kv_compact(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_status),
+                                _ptr(d_ws), _bytes(d_ws), _stream(stream)), "vq_kv_compact")
+
+
+def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None) -> None:
+    _here(d_pairs)
+    _check(load().vq_kv_copy_pages(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), _ptr(d_pairs), int(n_pairs), _stream(stream)),
+           "vq_kv_copy_pages")
+
+
+def vq_residual_norm(norm: VQNorm, d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h, stream=None) -> None:
+    """x' = x + residual_scale * gate * post(y), h = pre(x'); absent operands are None."""
+    operands = (d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h)
+    _here(*operands)
+    _check(load().vq_residual_norm(ctypes.byref(norm.c()), *[_ptr(t) for t in operands], _stream(stream)), "vq_residual_norm")

@@ -1,0 +1,742 @@
+"""Paged cache, its attention and the residual norm on the GPU against plain 64-bit definitions.
+
+Tolerances.  A result is rounded once: half a step, eps / 2 of its type (2^-11 of a binary16 value, 2^-24 of a binary32
+one, 2^-25 absolute where binary16 is subnormal).  Sums are binary32: a sum of n products of magnitude A is off by less
+than n * 2^-23 * A however it is ordered (the tensor cores drop bits, so a whole step each).  A score that is off by ds
+changes a weight by the factor exp(ds), numerator and denominator each.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2402_15319_b200 as vq
+from tests import kv_ref
+from tests.helpers import assert_guards_intact, guarded
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+HALF, SUB = 2.0 ** -11, 2.0 ** -25
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2402_15319_b200 import build
+    build.build()
+
+
+def fill(rng, int8, shape):
+    """A pool with its scales, all of it ordinary numbers."""
+    if not int8:
+        return torch.from_numpy(rng.standard_normal(shape).astype(np.float16)), None
+    return (torch.from_numpy(rng.integers(-127, 128, shape).astype(np.int8)),
+            torch.from_numpy(rng.uniform(0.004, 0.03, shape[:-1]).astype(np.float32)))
+
+
+class Cache:
+    """Host copies of a random cache: lens given, pages scattered, everything that no token lives in poisoned."""
+
+    def __init__(self, lens, heads, dim, page, int8, seed, slack=3, extra_stride=1, poison=True):
+        rng = np.random.default_rng(seed)
+        need = [-(-max(n, 0) // page) for n in lens]
+        self.n_pages = sum(need) + slack
+        stride = max(1, max(need)) + extra_stride
+        order = rng.permutation(self.n_pages)
+        self.table = torch.full((len(lens), stride), -7, dtype=torch.int32)
+        at = 0
+        for s, c in enumerate(need):
+            self.table[s, :c] = torch.from_numpy(order[at:at + c].astype(np.int32))
+            at += c
+        self.len = torch.tensor(lens, dtype=torch.int32)
+        self.fmt = vq.VQKVFormat(self.n_pages, page, heads, dim, vq.VQ_KV_INT8 if int8 else vq.VQ_KV_FP16)
+        shape = (self.n_pages, heads, page, dim)
+        (self.k, self.ks), (self.v, self.vs) = fill(rng, int8, shape), fill(rng, int8, shape)
+        if poison:
+            live = torch.zeros(self.n_pages, page, dtype=torch.bool)
+            for s, n in enumerate(lens):
+                for t in range(max(n, 0)):
+                    live[int(self.table[s, t // page]), t % page] = True
+            dead = ~live[:, None, :].expand(self.n_pages, heads, page)
+            for pool, scale in ((self.k, self.ks), (self.v, self.vs)):
+                if scale is None:
+                    pool[dead] = float("nan")
+                else:
+                    scale[dead] = float("nan")
+
+    def device(self):
+        to = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+        return vq.KVPool(to(self.k), to(self.v), to(self.ks), to(self.vs)), vq.KVSeqs(self.table.to(DEV), self.len.to(DEV))
+
+
+def workspace(fmt):
+    return torch.zeros(vq.vq_kv_attention_workspace_bytes(fmt), dtype=torch.uint8, device=DEV)
+
+
+def attend(cache, q, scale, window=0, ws=None, dev=None, lse=True):
+    """out, lse on the host; rows of q and out wider than the heads, guards checked."""
+    n, hq, d = q.shape
+    pool, seqs = dev or cache.device()
+    ws = workspace(cache.fmt) if ws is None else ws
+    qd = torch.full((n, hq * d + 24), float("nan"), dtype=torch.float16, device=DEV)
+    qd[:, :hq * d] = q.reshape(n, -1).to(DEV)
+    out, raw = guarded((n, hq * d + 16), torch.float16, DEV, fill=77.0)
+    ls, raw_l = guarded((n, hq), torch.float32, DEV)
+    vq.vq_kv_attention(cache.fmt, pool, seqs, hq, qd, hq * d + 24, out, hq * d + 16, ls if lse else None, scale, window, ws)
+    torch.cuda.synchronize()
+    assert_guards_intact(raw, "out")
+    assert_guards_intact(raw_l, "lse")
+    assert bool((out[:, hq * d:] == 77.0).all()), "columns between the rows were written"
+    assert int(ws[:2048].view(torch.int32).abs().sum()) == 0, "the counters are left as they were found"
+    return out[:, :hq * d].reshape(n, hq, d).cpu(), ls.cpu()
+
+
+def check(cache, q, out, lse, scale, window=0):
+    ref, ref_l, mag, ds = kv_ref.attention(q, cache.k, cache.v, cache.ks, cache.vs, cache.table, cache.len, cache.fmt.page_tokens, scale, window)
+    d, n_max = q.shape[2], int(cache.len.max())
+    # score: d products, then scale (8-bit: two factors) in binary32, and the exponential's argument (|score| up to ds * log2 e
+    # rounded twice) and its own 2^-22; weights: numerator and denominator; sums over at most n_max tokens and their joins
+    e = 2 * ((d + 8) * 2.0 ** -23 * ds + 2.0 ** -20) + (n_max + 64) * 2.0 ** -23 + 2.0 ** -21
+    tol = HALF * ref.abs() + SUB + e[..., None] * mag * (1 + HALF)
+    bad = (out.double() - ref).abs() > tol
+    assert not bool(bad.any()), f"{int(bad.sum())} off, worst {float(((out.double() - ref).abs() / tol).max())}"
+    empty = torch.isinf(ref_l)
+    assert torch.equal(empty, torch.isinf(lse)) and bool((lse[empty] < 0).all()) and bool((out[empty] == 0).all())
+    tol_l = (d + 8) * 2.0 ** -23 * ds + (n_max + 64) * 2.0 ** -23 + 2.0 ** -20 + 2.0 ** -22 * ref_l.abs()
+    assert bool(((lse.double() - ref_l).abs()[~empty] <= tol_l[~empty]).all())
+
+
+def queries(n, hq, d, seed):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal((n, hq, d)).astype(np.float16))
+
+
+LENS = [0, 1, 7, 8, 9, 15, 16, 17, 31, 33, 63, 64, 65, 127, 130, 257, 0, 300]
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("dim,heads,group,page", [
+    (128, 2, 4, 16), (64, 3, 8, 8), (80, 1, 5, 32), (96, 2, 1, 64), (192, 1, 16, 16), (256, 2, 2, 128), (128, 1, 9, 256), (64, 1, 20, 16), (128, 8, 1, 16),
+    (256, 1, 33, 8),
+])
+def test_attention_shapes(dim, heads, group, page, int8):
+    c = Cache(LENS, heads, dim, page, int8, seed=dim + group)
+    q = queries(len(LENS), heads * group, dim, 5)
+    check(c, q, *attend(c, q, dim ** -0.5), dim ** -0.5)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("window", [1, 5, 16, 64, 100, 1 << 30])
+def test_attention_window(window, int8):
+    c = Cache(LENS, 2, 64, 8, int8, seed=window % 97)
+    q = queries(len(LENS), 6, 64, 6)
+    check(c, q, *attend(c, q, 0.2, window), 0.2, window)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lens", [[1], [40000], [20000, 3, 0, 9000], [700] * 40, [0] * 5, [0] * 200 + [5]])
+def test_attention_splits(lens, int8):
+    """One sequence over every CTA, pieces of many sequences in one CTA, nothing at all, more sequences than threads."""
+    c = Cache(lens, 1, 64, 16, int8, seed=len(lens), poison=max(lens) < 5000)
+    q = queries(len(lens), 2, 64, 7)
+    check(c, q, *attend(c, q, 0.125), 0.125)
+
+
+def test_attention_many_short():
+    rng = np.random.default_rng(3)
+    lens = [int(n) for n in rng.integers(0, 40, 700)]
+    c = Cache(lens, 2, 64, 8, False, seed=8)
+    q = queries(len(lens), 4, 64, 8)
+    check(c, q, *attend(c, q, 0.125), 0.125)
+
+
+def test_attention_stored_lengths_out_of_range():
+    """A negative length is none, one beyond the table is the table's."""
+    c = Cache([32, 32, 32], 1, 64, 16, False, seed=1, extra_stride=0)
+    q = queries(3, 2, 64, 9)
+    c.len = torch.tensor([-5, 1 << 30, 32], dtype=torch.int32)
+    out, lse = attend(c, q, 0.125)
+    c.len = torch.tensor([0, 32, 32], dtype=torch.int32)
+    check(c, q, out, lse, 0.125)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_bad_pages(int8):
+    """Tokens whose table entry names no page of the pool do not take part."""
+    c = Cache([100, 64, 16, 40], 2, 128, 16, int8, seed=4)
+    c.table[0, 2], c.table[1, 0], c.table[2, 0], c.table[3, 2] = -1, c.n_pages, 2 ** 31 - 1, -2 ** 31
+    q = queries(4, 8, 128, 10)
+    check(c, q, *attend(c, q, 0.1), 0.1)
+
+
+def test_attention_large_and_small_scores():
+    """Scores to the hundreds (weights of 0 and 1), weights far below the largest, one key that takes all."""
+    c = Cache([500, 500, 90], 1, 128, 16, False, seed=5, poison=False)
+    c.k[int(c.table[0, 3]), 0, 5] *= 30
+    c.v *= 100
+    q = queries(3, 4, 128, 11)
+    check(c, q, *attend(c, q, 4.0), 4.0)
+    check(c, q, *attend(c, q, 1e-4), 1e-4)
+    check(c, q, *attend(c, q, -0.3), -0.3)
+
+
+def test_attention_many_small_weights_count():
+    """20000 weights of 2^-27 of the largest each: together they move the result by 1.5e-4, and none may be dropped."""
+    n, d = 20001, 64
+    c = Cache([n], 1, d, 256, False, seed=6, poison=False)
+    c.k.zero_()
+    c.k[int(c.table[0, 0]), 0, 0, 0] = 1.0
+    c.v.fill_(1024.0)
+    c.v[int(c.table[0, 0]), 0, 0] = 0.0
+    q = torch.zeros(1, 1, d, dtype=torch.float16)
+    q[0, 0, 0] = 27 * math.log(2)
+    out, lse = attend(c, q, 1.0)
+    check(c, q, out, lse, 1.0)
+    assert float(out[0, 0, 0]) > 0.1
+
+
+def test_attention_int8_scales():
+    """Value scales over forty powers of two, tokens whose values are all zero (scale 0) with the largest score."""
+    c = Cache([130, 64, 8], 1, 128, 16, True, seed=7, poison=False)
+    rng = np.random.default_rng(7)
+    c.vs = torch.from_numpy((2.0 ** rng.uniform(-34, 6, c.vs.shape)).astype(np.float32))
+    zero = int(c.table[0, 1])
+    c.v[zero, 0, 3], c.vs[zero, 0, 3], c.ks[zero, 0, 3] = 0, 0.0, 0.2
+    c.v[int(c.table[2, 0])], c.vs[int(c.table[2, 0])] = 0, 0.0      # a sequence of zeros
+    q = queries(3, 4, 128, 12)
+    check(c, q, *attend(c, q, 0.1), 0.1)
+
+
+def test_attention_nan_in_place_shows():
+    """A NaN that a token does have reaches its sequence and no other."""
+    c = Cache([40, 40], 1, 64, 16, False, seed=8)
+    c.k[int(c.table[0, 1]), 0, 4, 7] = float("nan")
+    q = queries(2, 2, 64, 13)
+    out, _ = attend(c, q, 0.1)
+    assert bool(torch.isnan(out[0]).all()) and not bool(torch.isnan(out[1]).any())
+
+
+def test_attention_same_bits_any_workspace_history():
+    c = Cache([5000, 77, 1234], 2, 128, 16, False, seed=9, poison=False)
+    other = Cache([900, 3], 1, 256, 32, True, seed=10)
+    q, q2 = queries(3, 8, 128, 14), queries(2, 3, 256, 15)
+    ws = torch.zeros(max(vq.vq_kv_attention_workspace_bytes(c.fmt), vq.vq_kv_attention_workspace_bytes(other.fmt)), dtype=torch.uint8, device=DEV)
+    first, l1 = attend(c, q, 0.1, ws=ws)
+    check(other, q2, *attend(other, q2, 0.1, ws=ws), 0.1)
+    again, l2 = attend(c, q, 0.1, ws=ws, lse=True)
+    assert torch.equal(first, again) and torch.equal(l1, l2)
+    without, _ = attend(c, q, 0.1, ws=ws, lse=False)
+    assert torch.equal(first, without)
+
+
+def test_attention_captured_replayed_with_other_lengths():
+    """One graph serves a growing cache: lengths and tables are read when it runs."""
+    c = Cache([600, 300], 2, 64, 16, False, seed=11)
+    pool, seqs = c.device()
+    q = queries(2, 4, 64, 16)
+    qd, ws = q.reshape(2, -1).to(DEV), workspace(c.fmt)
+    out, lse = torch.empty(2, 256, dtype=torch.float16, device=DEV), torch.empty(2, 4, device=DEV)
+    call = lambda: vq.vq_kv_attention(c.fmt, pool, seqs, 4, qd, 256, out, 256, lse, 0.1, 0, ws)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+        call()
+    for lens in ([600, 300], [1, 0], [599, 17]):
+        c.len = torch.tensor(lens, dtype=torch.int32)
+        seqs.length.copy_(c.len)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(c, q, out.view(2, 4, 64).cpu(), lse.cpu(), 0.1)
+
+
+def test_attention_two_streams_two_workspaces():
+    caches = [Cache([3000, 50], 2, 128, 16, False, seed=s, poison=False) for s in (12, 13)]
+    q = queries(2, 8, 128, 17)
+    alone = [attend(c, q, 0.1)[0] for c in caches]
+    dev, streams = [c.device() for c in caches], [torch.cuda.Stream(DEV) for _ in caches]
+    qd = q.reshape(2, -1).to(DEV)
+    outs, wss = [torch.empty(2, 1024, dtype=torch.float16, device=DEV) for _ in caches], [workspace(c.fmt) for c in caches]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, (pool, seqs), st, out, ws in zip(caches, dev, streams, outs, wss):
+            vq.vq_kv_attention(c.fmt, pool, seqs, 8, qd, 1024, out, 1024, None, 0.1, 0, ws, stream=st)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, outs):
+        assert torch.equal(a, b.view(2, 8, 128).cpu())
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_offsets_beyond_32_bits(int8):
+    """Pages whose byte offset in the pool passes 2^32 (2^33 for binary16)."""
+    heads, page, dim = 8, 64, 128
+    n_pages = (1 << 33) // (heads * page * dim * 2) + 40 if not int8 else (1 << 32) // (heads * page * dim) + 40
+    fmt = vq.VQKVFormat(n_pages, page, heads, dim, vq.VQ_KV_INT8 if int8 else vq.VQ_KV_FP16)
+    shape = (n_pages, heads, page, dim)
+    pool = vq.KVPool(*[torch.empty(shape, dtype=torch.int8 if int8 else torch.float16, device=DEV) for _ in range(2)],
+                     *([torch.empty(shape[:3], dtype=torch.float32, device=DEV) for _ in range(2)] if int8 else [None, None]))
+    c = Cache([130, 64], heads, dim, page, int8, seed=14)
+    at = torch.arange(c.n_pages, device=DEV) + (n_pages - c.n_pages)
+    for big, small in zip(pool, (c.k, c.v, c.ks, c.vs)):
+        if big is not None:
+            big[at] = small.to(DEV)
+    seqs = vq.KVSeqs((c.table + (n_pages - c.n_pages)).to(DEV), c.len.to(DEV))
+    q = queries(2, 16, dim, 18)
+    small_fmt, c.fmt = c.fmt, fmt
+    out, lse = attend(c, q, 0.1, dev=(pool, seqs))
+    c.fmt = small_fmt
+    check(c, q, out, lse, 0.1)
+
+
+# ---- append -------------------------------------------------------------------------------------------------------
+
+def rope_table(n, rot, seed=0):
+    at = np.arange(n, dtype=np.float64) + 1000.0 * seed
+    freq = 10000.0 ** (-np.arange(rot // 2) / (rot // 2))
+    ang = at[:, None] * freq[None]
+    return torch.from_numpy(np.stack([np.cos(ang), np.sin(ang)], -1).astype(np.float32))
+
+
+def run_append(c, starts, k, v, q, cs, rot, interleaved, in_place=False):
+    """Appends on the GPU; pools and rotated queries back on the host."""
+    pool, seqs = c.device()
+    n, hk, d = k.shape
+    hq = 0 if q is None else q.shape[1]
+    row = torch.full((n, (hq + 2 * hk) * d + 8), float("nan"), dtype=torch.float16, device=DEV)   # as a fused projection gives it
+    if hq:
+        row[:, :hq * d] = q.reshape(n, -1).to(DEV)
+    row[:, hq * d:(hq + hk) * d] = k.reshape(n, -1).to(DEV)
+    row[:, (hq + hk) * d:(hq + 2 * hk) * d] = v.reshape(n, -1).to(DEV)
+    qo = row if in_place else torch.full((n, max(8, hq * d)), 77.0, dtype=torch.float16, device=DEV)
+    r = None
+    if rot:
+        r = vq.KVRotary(cs.to(DEV), cs.shape[0], rot, interleaved, hq, row if hq else None, row.stride(0), qo if hq else None, qo.stride(0))
+    vq.vq_kv_append(c.fmt, pool, seqs, None if starts is None else torch.tensor(starts, dtype=torch.int32, device=DEV), n, row[:, hq * d:], row.stride(0),
+                    row[:, (hq + hk) * d:], row.stride(0), r)
+    torch.cuda.synchronize()
+    back = [None if t is None else t.cpu() for t in pool]
+    return back, (qo[:, :hq * d].reshape(n, hq, d).cpu() if hq else None)
+
+
+def check_append(c, starts, k, v, q, cs, rot, interleaved, in_place=False):
+    (k2, v2, ks2, vs2), qo = run_append(c, starts, k, v, q, cs, rot, interleaved, in_place)
+    n, hk, d = k.shape
+    page = c.fmt.page_tokens
+    touched = torch.zeros(c.n_pages, page, dtype=torch.bool)
+    st = starts if starts is not None else list(range(len(c.len) + 1))
+    for s in range(len(c.len)):
+        for j in range(st[s], st[s + 1]):
+            pos = int(c.len[s]) - st[s + 1] + j
+            if pos < 0:
+                continue
+            where = int(c.table[s, pos // page])
+            turn = cs[pos] if rot else torch.zeros(0, 2)
+            if q is not None and rot:
+                exact = kv_ref.rotate(q[j].double(), turn, rot, interleaved)
+                size = kv_ref.rotate(q[j].double().abs(), torch.stack([turn[:, 0].abs(), -turn[:, 1].abs()], -1), rot, interleaved).abs() + q[j].double().abs()
+                # two products and a sum in binary32, then half a step
+                assert bool(((qo[j].double() - exact).abs() <= HALF * exact.abs() + SUB + 3 * 2.0 ** -24 * 2 * size).all())
+            if not 0 <= where < c.n_pages:
+                continue
+            touched[where, pos % page] = True
+            for new, pool, scale, turned in ((k, k2, ks2, True), (v, v2, vs2, False)):
+                exact = kv_ref.rotate(new[j].double(), turn, rot if turned else 0, interleaved)
+                got = pool[where, :, pos % page].double()
+                slop = 12 * 2.0 ** -24 * new[j].double().abs().amax(-1, keepdim=True)
+                if scale is None:
+                    assert bool(((got - exact).abs() <= (HALF * exact.abs() + SUB + slop if turned and rot else 0.0)).all())
+                    continue
+                step = scale[where, :, pos % page].double()[:, None]
+                top = exact.abs().amax(-1, keepdim=True)
+                assert bool(((step - top / 127).abs() <= 2.0 ** -22 * top / 127 + slop).all())
+                # half a step of the 8-bit grid (the quotient is rounded to 24 bits first)
+                assert bool(((got * step - exact).abs() <= step * (0.5 + 127 * 2.0 ** -23) + 2 * slop).all())
+    for old, new in ((c.k, k2), (c.v, v2), (c.ks, ks2), (c.vs, vs2)):   # nothing else is written
+        if old is not None:
+            keep = ~touched[:, None, :].expand(*old.shape[:3])
+            assert torch.equal(old[keep].contiguous().view(torch.uint8), new[keep].contiguous().view(torch.uint8))
+    if q is not None and rot and starts is not None and starts[-1] < n:
+        rest = qo[starts[-1]:]
+        assert torch.equal(rest, q[starts[-1]:]) if in_place else bool((rest == 77.0).all())   # rows behind the last sequence
+
+
+def rows(n, h, d, seed):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal((n, h, d)).astype(np.float16))
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("dim,hk,group,page,rot,interleaved", [
+    (128, 2, 4, 16, 128, 0), (64, 3, 2, 8, 64, 1), (80, 1, 3, 32, 32, 0), (96, 2, 1, 64, 48, 1), (256, 1, 2, 16, 256, 0), (16, 2, 2, 8, 16, 1), (192, 1, 5, 8, 96, 0),
+    (48, 2, 3, 16, 0, 0), (240, 1, 2, 128, 240, 1),
+])
+def test_append_packed(dim, hk, group, page, rot, interleaved, int8):
+    """Packed prompts: empty ones between, continued ones, rows behind the last."""
+    new, before = [5, 0, 1, 40, 0, 17, 3], [0, 9, 15, 7, 0, 33, 300]
+    c = Cache([a + b for a, b in zip(new, before)], hk, dim, page, int8, seed=dim + rot)
+    starts = [0] + list(np.cumsum(new))
+    n = starts[-1] + 4
+    cs = rope_table(c.table.shape[1] * page, rot, seed=2) if rot else None
+    check_append(c, [int(s) for s in starts], rows(n, hk, dim, 1), rows(n, hk, dim, 2), rows(n, hk * group, dim, 3), cs, rot, interleaved)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lens", [[1], [1, 16, 17, 0, 64, 5], [3] * 150])
+def test_append_one_each(lens, int8):
+    c = Cache(lens, 2, 128, 16, int8, seed=len(lens))
+    cs = rope_table(c.table.shape[1] * 16, 128)
+    n = len(lens)
+    check_append(c, None, rows(n, 2, 128, 4), rows(n, 2, 128, 5), rows(n, 8, 128, 6), cs, 128, 0, in_place=True)
+    check_append(c, None, rows(n, 2, 128, 4), rows(n, 2, 128, 5), None, rope_table(c.table.shape[1] * 16, 64), 64, 1)      # keys only
+
+
+def test_append_thousand_sequences_and_bad_pages():
+    rng = np.random.default_rng(5)
+    new = [int(x) for x in rng.integers(0, 4, 1100)]
+    c = Cache([a + int(b) for a, b in zip(new, rng.integers(0, 20, 1100))], 1, 64, 8, False, seed=15)
+    for s in range(0, 1100, 37):
+        c.table[s] = torch.tensor([-1, c.n_pages, 2 ** 31 - 1, 0])[s % 3]
+    starts = [0] + [int(x) for x in np.cumsum(new)]
+    n = starts[-1]
+    check_append(c, starts, rows(n, 1, 64, 7), rows(n, 1, 64, 8), rows(n, 2, 64, 9), rope_table(c.table.shape[1] * 8, 64), 64, 0)
+
+
+def test_append_starts_and_lengths_that_disagree():
+    """More new tokens than the sequence has: those in front of its first place are dropped."""
+    c = Cache([4, 40], 1, 64, 8, False, seed=16)
+    check_append(c, [0, 10, 12], rows(12, 1, 64, 1), rows(12, 1, 64, 2), None, None, 0, 0)
+
+
+def test_append_int8_odd_rows():
+    """Zeros, infinities, NaN, the smallest and the largest numbers in 8-bit rows."""
+    c = Cache([5], 1, 64, 8, True, seed=17)
+    k = rows(5, 1, 64, 1)
+    k[0], k[1, 0, 3], k[2, 0, 5] = 0.0, float("inf"), float("nan")
+    k[3], k[4] = 2.0 ** -24, 65504.0
+    k[3, 0, ::2] = 0.0
+    (k2, v2, ks2, vs2), _ = run_append(c, [0, 5], k, rows(5, 1, 64, 2), None, None, 0, 0)
+    got = (k2.double() * ks2.double()[..., None])[int(c.table[0, 0]), 0]
+    assert bool((got[0] == 0).all()) and bool(torch.isnan(got[1:3]).all())
+    assert torch.allclose(got[3], k[3, 0].double(), rtol=2.0 ** -20, atol=0) and torch.allclose(got[4], k[4, 0].double(), rtol=2.0 ** -20, atol=0)
+
+
+# ---- pages ----------------------------------------------------------------------------------------------------------
+
+class DeviceBooks:
+    def __init__(self, model, layers, heads, dim, int8, seed):
+        rng = np.random.default_rng(seed)
+        self.m = model
+        self.fmt = vq.VQKVFormat(model.n_pages, model.page, heads, dim, vq.VQ_KV_INT8 if int8 else vq.VQ_KV_FP16)
+        shape = (model.n_pages, heads, model.page, dim)
+        self.host = [[*fill(rng, int8, shape), *fill(rng, int8, shape)] for _ in range(layers)]   # k, ks, v, vs
+        to = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+        self.pools = [vq.KVPool(to(k), to(v), to(ks), to(vs)) for k, ks, v, vs in self.host]
+        n, w = len(model.len), model.stride
+        self.raw = torch.full((n * w + n + model.n_pages + 2 + 64,), 12345, dtype=torch.int32, device=DEV)   # 4-byte aligned pieces, a guard behind
+        self.table, self.len = self.raw[:n * w].view(n, w), self.raw[n * w:n * w + n]
+        self.refs = self.raw[n * w + n:n * w + n + model.n_pages]
+        self.status = self.raw[n * w + n + model.n_pages:][:2]
+        self.push()
+        self.ws = torch.full((vq.vq_kv_pages_workspace_bytes(self.fmt, n),), 0xA5, dtype=torch.uint8, device=DEV)
+        self.seqs = vq.KVSeqs(self.table, self.len)
+
+    def push(self):
+        self.table.copy_(torch.tensor(self.m.table, dtype=torch.int32))
+        self.len.copy_(torch.tensor(self.m.len, dtype=torch.int32))
+        self.refs.copy_(torch.tensor(self.m.refs, dtype=torch.int32))
+
+    def ints(self, x):
+        return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+    def same(self, status=None, copies=()):
+        torch.cuda.synchronize()
+        assert self.table.cpu().tolist() == self.m.table and self.len.cpu().tolist() == self.m.len and self.refs.cpu().tolist() == self.m.refs
+        if status is not None:
+            assert tuple(self.status.cpu().tolist()) == tuple(status)
+        assert bool((self.raw[-64:] == 12345).all())
+        for pools, host in zip(self.pools, self.host):
+            for dev, h in zip((pools.k, pools.k_scale, pools.v, pools.v_scale), host):
+                if h is None:
+                    continue
+                old = h.clone()
+                for src, dst, tokens in copies:
+                    h[dst, :, :tokens] = old[src, :, :tokens]
+                assert torch.equal(dev.cpu().view(torch.uint8), h.view(torch.uint8))
+
+    def reserve(self, grow=None):
+        vq.vq_kv_reserve(self.fmt, self.seqs, self.refs, None if grow is None else self.ints(grow), self.status, self.ws)
+        self.same(self.m.reserve([1] * len(self.m.len) if grow is None else grow))
+
+    def fork(self, pairs):
+        vq.vq_kv_fork(self.fmt, self.pools, self.seqs, self.refs, self.ints(pairs), len(pairs), self.status, self.ws)
+        self.same(*self.m.fork(pairs))
+
+    def free(self, slots):
+        vq.vq_kv_free(self.fmt, self.seqs, self.refs, self.ints(slots), len(slots))
+        self.m.free(slots)
+        self.same()
+
+    def compact(self):
+        vq.vq_kv_compact(self.fmt, self.pools, self.seqs, self.refs, self.status, self.ws)
+        self.same(*self.m.compact())
+
+
+@pytest.mark.parametrize("n_pages,page,n_seqs,stride,layers,heads,dim,int8", [
+    (1, 8, 1, 1, 1, 1, 16, False), (31, 8, 5, 6, 2, 2, 64, False), (33, 16, 7, 5, 1, 3, 80, True), (257, 8, 20, 40, 3, 1, 48, True),
+    (1000, 16, 40, 30, 1, 1, 16, False), (64, 64, 6, 20, 2, 2, 128, False),
+])
+def test_books_random_walk(n_pages, page, n_seqs, stride, layers, heads, dim, int8):
+    """Reserve, fork, free and compact in random order, failures and bad entries among them: equal to the rules, always."""
+    rng = np.random.default_rng(n_pages)
+    d = DeviceBooks(kv_ref.Books(n_pages, page, n_seqs, stride), layers, heads, dim, int8, seed=n_pages)
+    mean = n_pages * page // n_seqs
+    for step in range(40):
+        what = rng.choice(["reserve", "reserve", "one", "fork", "free", "compact"])
+        if what == "reserve":
+            grow = rng.integers(-2, max(2, mean // 2), n_seqs) * (rng.random(n_seqs) < 0.4)
+            d.reserve([int(x) for x in grow])
+        elif what == "one":
+            d.reserve()
+        elif what == "fork":
+            n = int(rng.integers(1, 2 * n_seqs + 1))
+            d.fork([[int(a), int(b)] for a, b in rng.integers(-1, n_seqs + 1, (n, 2))])
+        elif what == "free":
+            d.free([int(x) for x in rng.integers(-1, n_seqs + 2, int(rng.integers(1, n_seqs + 1)))])
+        else:
+            d.compact()
+
+
+def test_books_large():
+    """Every thread of the counting CTA has pages, every copying warp has runs; a page of several runs."""
+    d = DeviceBooks(kv_ref.Books(40007, 8, 300, 2500), 1, 1, 16, False, seed=1)
+    rng = np.random.default_rng(1)
+    d.reserve([int(x) for x in rng.integers(0, 1800, 300)])
+    d.free([int(x) for x in rng.permutation(300)[:120]])
+    empty = [s for s in range(300) if d.m.len[s] == 0]
+    live = [s for s in range(300) if d.m.len[s]]
+    d.fork([[live[i % len(live)], e] for i, e in enumerate(empty[:100])])
+    d.free(live[::3])
+    d.compact()
+    d.reserve([8 * 2500 - n for n in d.m.len])      # the whole of every row: far more than there is
+    d = DeviceBooks(kv_ref.Books(20, 64, 4, 12), 2, 8, 128, False, seed=2)
+    d.reserve([700, 64, 0, 1])
+    d.fork([[0, 2]])
+    d.free([0, 1])
+    d.compact()
+    d.compact()
+    d.reserve([0, 64 * 12 + 1, 0, 0])               # one row too short
+
+
+def test_fork_many_entries_and_free_repeated():
+    d = DeviceBooks(kv_ref.Books(3000, 8, 1100, 10), 1, 1, 16, True, seed=3)
+    d.reserve([20, 0, 16] + [0] * 1097)
+    d.fork([[i % 3, 3 + i] for i in range(1024)])
+    d.free([5, 5, 5, 0, -1, 1100, 2 ** 31 - 1, -2 ** 31, 0])
+    d.reserve()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_copy_pages(int8):
+    m = kv_ref.Books(50, 16, 1, 1)
+    d = DeviceBooks(m, 3, 5, 80, int8, seed=4)
+    pairs = [[0, 49], [0, 7], [3, 8], [-1, 9], [10, 50], [2 ** 31 - 1, 11], [12, -5], [13, 13]]
+    vq.vq_kv_copy_pages(d.fmt, d.pools, d.ints(pairs), len(pairs))
+    d.same(copies=[(0, 49, 16), (0, 7, 16), (3, 8, 16)])
+
+
+def test_pages_in_a_graph():
+    """A captured step that takes a page when it needs one: replayed, it goes on where the books are."""
+    d = DeviceBooks(kv_ref.Books(20, 8, 2, 8), 1, 1, 16, False, seed=5)
+    d.reserve([7, 3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vq.vq_kv_reserve(d.fmt, d.seqs, d.refs, None, d.status, d.ws)
+    for _ in range(12):
+        graph.replay()
+        d.same(d.m.reserve([1, 1]))
+
+
+# ---- residual norm ------------------------------------------------------------------------------------------------------
+
+def norm_ref(x, layer, w, b, eps):
+    """The norm in 64 bits and a bound of its binary32 evaluation's error, from |x| alone."""
+    n = x.shape[1]
+    c = x - x.mean(1, keepdim=True) if layer else x
+    r = 1 / (c.square().mean(1, keepdim=True) + eps).sqrt()
+    y = c * r * w
+    # mean and centred values: n additions of |x| (relative to the largest), the sum of squares and the root relative to r
+    e = (n + 8) * 2.0 ** -24 * 2
+    slop = e * (y.abs() + (r * w.abs() * x.abs().mean(1, keepdim=True) * 3 if layer else 0))
+    if layer:   # the mean's error shifts every value: its square's change is of second order but for eps
+        slop = slop + e * (c.abs() * r * w.abs()) * (r * x.abs().mean(1, keepdim=True))
+    if b is not None:
+        y, slop = y + b, slop + 2.0 ** -23 * (y.abs() + b.abs())
+    return y, slop
+
+
+@pytest.mark.parametrize("layer,post,gate,wide", [
+    (False, False, 0, False), (True, True, 1, True), (False, True, 2, False), (True, False, 2, True), (False, True, 1, True), (True, True, 0, False),
+])
+@pytest.mark.parametrize("n_rows,n_cols", [(1, 1), (3, 7), (5, 8), (9, 100), (2, 256), (7, 257), (3, 264), (1, 4096), (4, 4100), (300, 512), (2, 8192), (150, 1000), (2, 32768), (1, 32767)])
+def test_norm(n_rows, n_cols, layer, post, gate, wide):
+    rng = np.random.default_rng(n_rows * 1000 + n_cols)
+    half = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float16))  # noqa: E731
+    pad = lambda k: n_cols + k  # noqa: E731
+    xt = torch.float32 if wide else torch.float16
+    x, y, g = half(n_rows, n_cols).to(xt) * 2 + 0.5, half(n_rows, n_cols) + 1, half(n_rows, n_cols) if gate == 2 else half(1, n_cols)
+    pw, pb, w, b = half(n_cols), half(n_cols), half(n_cols), half(n_cols)
+    strides = [pad(8), pad(16), pad(24), pad(32), pad(40)]
+
+    def wide_rows(t, stride):
+        d = torch.full((t.shape[0], stride), float("nan"), dtype=t.dtype, device=DEV)
+        d[:, :n_cols] = t.to(DEV)
+        return d
+
+    dx, dy, dg = wide_rows(x, strides[0]), wide_rows(y, strides[1]), wide_rows(g, strides[2])
+    out, raw1 = guarded((n_rows, strides[3]), xt, DEV, fill=55.0)
+    h, raw2 = guarded((n_rows, strides[4]), torch.float16, DEV, fill=55.0)
+    scale, eps = 0.7, 1e-5
+    nb = vq.VQNorm(n_rows, n_cols, int(layer), int(wide), gate, eps, scale, *strides)
+    to = lambda t: t.to(DEV)  # noqa: E731
+    vq.vq_residual_norm(nb, dx, dy, dg if gate else None, to(pw) if post else None, to(pb) if post and layer else None, to(w), to(b) if layer else None, out, h)
+    torch.cuda.synchronize()
+    assert_guards_intact(raw1, "x_out")
+    assert_guards_intact(raw2, "h")
+    assert bool((out[:, n_cols:] == 55.0).all()) and bool((h[:, n_cols:] == 55.0).all())
+    f32 = lambda v: float(np.float32(v))  # noqa: E731
+    u, su = y.double(), torch.zeros(n_rows, n_cols, dtype=torch.float64)
+    if post:
+        u, su = norm_ref(u, layer, pw.double(), pb.double() if layer else None, f32(eps))
+    gg = g.double() if gate else torch.ones(1, n_cols, dtype=torch.float64)
+    add = f32(scale) * gg * u
+    want = x.double() + add
+    sx = f32(scale) * gg.abs() * su + 4 * 2.0 ** -24 * (add.abs() + want.abs())
+    lost = 2.0 ** -24 if wide else HALF
+    got = out[:, :n_cols].cpu().double()
+    assert bool(((got - want).abs() <= lost * want.abs() + SUB + sx).all())
+    ref, sh = norm_ref(want, layer, w.double(), b.double() if layer else None, f32(eps))
+    c = want - want.mean(1, keepdim=True) if layer else want
+    r = 1 / (c.square().mean(1, keepdim=True) + f32(eps)).sqrt()
+    # x' is off by sx: directly, through the mean, and through the root of the mean square
+    worst = sx + sx.mean(1, keepdim=True)
+    sh = sh + r * w.double().abs() * (worst + c.abs() * r * r * (c.abs() * worst).mean(1, keepdim=True))
+    got = h[:, :n_cols].cpu().double()
+    tol = HALF * ref.abs() + SUB + 2 * sh
+    assert bool(((got - ref).abs() <= tol).all()), float(((got - ref).abs() / tol).max())
+
+
+@pytest.mark.parametrize("n_cols", [96, 5000])
+def test_norm_parts_and_places(n_cols):
+    """Without a block's output, without a norm behind, in place, h over y, captured."""
+    rng = np.random.default_rng(n_cols)
+    x, y, w = (torch.from_numpy(rng.standard_normal((6, n_cols)).astype(np.float16)).to(DEV) for _ in range(3))
+    w = w[0].contiguous()
+    nb = vq.VQNorm(6, n_cols, vq.VQ_NORM_RMS, vq.VQ_RESIDUAL_FP16, vq.VQ_GATE_NONE, 1e-6, 1.0, n_cols, n_cols, 0, n_cols, n_cols)
+    h = torch.empty_like(x)
+    vq.vq_residual_norm(nb, x, None, None, None, None, w, None, None, h)          # the first norm of a model
+    ref, slop = norm_ref(x.cpu().double(), False, w.cpu().double(), None, 1e-6)
+    assert bool(((h.cpu().double() - ref).abs() <= HALF * ref.abs() + SUB + 2 * slop).all())
+    out = torch.empty_like(x)
+    vq.vq_residual_norm(nb, x, y, None, None, None, None, None, out, None)        # the last sum
+    assert torch.equal(out, (x.float() + y.float()).half())
+    vq.vq_residual_norm(nb, x, y, None, None, None, w, None, out, h)
+    x2, y2 = x.clone(), y.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vq.vq_residual_norm(nb, x2, y2, None, None, None, w, None, x2, y2)        # in place, h over y
+    x2.copy_(x)
+    y2.copy_(y)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(x2, out) and torch.equal(y2, h)
+
+
+# ---- a decode step ---------------------------------------------------------------------------------------------------------
+
+def test_decode_steps_of_a_block():
+    """Norm, q/k/v in one grouped product, pages reserved, keys turned and written, attention, output product, residual and
+    next norm, captured once and replayed for four tokens of three sequences; a fork and a compaction between.  Against
+    the same in 64 bits from the decoded weights, rounded where the calls round."""
+    import vq_synth
+    from oracle import vq_oracle as orc
+    from tests.helpers import DeviceLayer, draw
+    hidden, hq, hk, d, page, n = 512, 4, 2, 64, 8, 3
+    spec = lambda name, rows, cols: vq_synth.LayerSpec(name, N=rows, K=cols, d=2, b=6, Br=128, Bc=128, int8=False)  # noqa: E731
+    specs = [spec("q", hq * d, hidden), spec("k", hk * d, hidden), spec("v", hk * d, hidden), spec("o", hidden, hq * d)]
+    layers = [draw(sp, 77, i) for i, sp in enumerate(specs)]
+    dev = [DeviceLayer(sp, la) for sp, la in zip(specs, layers)]
+    W = [torch.from_numpy(dl.decode().astype(np.float64)) for dl in dev]
+    gfmt = vq.VQFormat(sum(sp.N for sp in specs[:3]), hidden, 2, 6, 128, 128, vq.VQ_CB_FP16)
+    fmt = vq.VQKVFormat(24, page, hk, d, vq.VQ_KV_FP16)
+    zeros = lambda *s, t=torch.float16: torch.zeros(s, dtype=t, device=DEV)  # noqa: E731
+    pool = vq.KVPool(zeros(24, hk, page, d), zeros(24, hk, page, d))
+    table, length, refs, status = zeros(n, 6, t=torch.int32), zeros(n, t=torch.int32), zeros(24, t=torch.int32), zeros(2, t=torch.int32)
+    seqs = vq.KVSeqs(table, length)
+    cs = rope_table(6 * page, d)
+    csd = cs.to(DEV)
+    ws = torch.zeros(vq.vq_workspace_bytes(gfmt, n), dtype=torch.uint8, device=DEV)
+    ws_o, ws_a = torch.zeros(vq.vq_workspace_bytes(dev[3].fmt, n), dtype=torch.uint8, device=DEV), workspace(fmt)
+    ws_p = torch.zeros(vq.vq_kv_pages_workspace_bytes(fmt, n), dtype=torch.uint8, device=DEV)
+    x, h, o, att = zeros(n, hidden, t=torch.float32), zeros(n, hidden), zeros(n, hidden), zeros(n, hq * d)
+    q, k, v = zeros(n, hq * d), zeros(n, hk * d), zeros(n, hk * d)
+    grow = zeros(n, t=torch.int32)
+    rng = np.random.default_rng(21)
+    w1, w2 = (torch.from_numpy((1 + 0.1 * rng.standard_normal(hidden)).astype(np.float16)) for _ in range(2))
+    w1d, w2d = w1.to(DEV), w2.to(DEV)
+    norm = vq.VQNorm(n, hidden, vq.VQ_NORM_RMS, vq.VQ_RESIDUAL_FP32, vq.VQ_GATE_NONE, 1e-5, 1.0, hidden, hidden, 0, hidden, hidden)
+    torch.cuda.synchronize()
+
+    def step():
+        vq.vq_residual_norm(norm, x, None, None, None, None, w1d, None, None, h)
+        vq.vq_gemm_small_batch_grouped(gfmt, [(dl.idx, dl.cb, dl.scale, y, sp.N) for dl, sp, y in zip(dev, specs, (q, k, v))], h, n, ws)
+        vq.vq_kv_reserve(fmt, seqs, refs, grow, status, ws_p)
+        vq.vq_kv_append(fmt, pool, seqs, None, n, k, hk * d, v, hk * d, vq.KVRotary(csd, 6 * page, d, 0, hq, q, hq * d, q, hq * d))
+        vq.vq_kv_attention(fmt, pool, seqs, hq, q, hq * d, att, hq * d, None, d ** -0.5, 0, ws_a)
+        vq.vq_gemm_small_batch(dev[3].fmt, dev[3].idx, dev[3].cb, dev[3].scale, att, o, n, ws_o)
+        vq.vq_residual_norm(norm, x, o, None, None, None, w2d, None, x, h)
+
+    step()      # (nothing grows: grow is 0, lengths are 0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    half = lambda t: t.to(torch.float16).double()  # noqa: E731
+    rms = lambda t, w: t / (t.square().mean(1, keepdim=True) + 1e-5).sqrt() * w.double()  # noqa: E731
+    keys, values = [[] for _ in range(n)], [[] for _ in range(n)]
+    active = [1, 1, 0]
+    for token in range(12):
+        if token == 10:    # the third sequence goes on from the first; the second ends, the pool closes up
+            vq.vq_kv_fork(fmt, [pool], seqs, refs, torch.tensor([[0, 2]], dtype=torch.int32, device=DEV), 1, status, ws_p)
+            vq.vq_kv_free(fmt, seqs, refs, torch.tensor([1], dtype=torch.int32, device=DEV), 1)
+            vq.vq_kv_compact(fmt, [pool], seqs, refs, status, ws_p)
+            keys[2], values[2] = list(keys[0]), list(values[0])
+            keys[1], values[1] = [], []
+            active = [1, 0, 1]
+        x0 = torch.from_numpy(rng.standard_normal((n, hidden)).astype(np.float32))
+        x.copy_(x0)
+        grow.copy_(torch.tensor(active, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert status.cpu().tolist()[0] == 0 or token == 10
+        hh = half(rms(x0.double(), w1))
+        qq, kk, vv = (half(hh @ w.T) for w in W[:3])
+        ctx = torch.zeros(n, hq * d, dtype=torch.float64)
+        for s in range(n):
+            if not active[s]:
+                continue
+            pos = len(keys[s])
+            turn = lambda t, m: half(kv_ref.rotate(t.view(m, d), cs[pos], d, 0))  # noqa: E731
+            keys[s].append(turn(kk[s], hk))
+            values[s].append(vv[s].view(hk, d))
+            K, V, Q = torch.stack(keys[s], 1), torch.stack(values[s], 1), turn(qq[s], hq).view(hk, hq // hk, d)
+            ctx[s] = (torch.softmax(Q @ K.transpose(1, 2) * d ** -0.5, -1) @ V).reshape(-1)
+        out = half(half(ctx) @ W[3].T)
+        want = x0.double() + out
+        on = torch.tensor(active, dtype=torch.bool)
+        # roundings to binary16 differ where 32 and 64 bits fall on two sides of a tie: a step in a few of the row's values
+        # (q, k, v, ctx, out), each scaled by the weights' row sums; a share of the result's size bounds them together
+        err = (x.cpu().double() - want)[on].abs().max() / out[on].abs().max()
+        assert float(err) < 0.02, (token, float(err))
+        ref = rms(want, w2)
+        assert float((h.cpu().double() - ref)[on].abs().max()) < 0.02 * float(ref[on].abs().max())
+    assert length.cpu().tolist() == [12, 0, 12]
+    assert sorted(p for p, r in enumerate(refs.cpu().tolist()) if r) == list(range(sum(1 for r in refs.cpu().tolist() if r)))

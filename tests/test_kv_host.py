@@ -1,0 +1,203 @@
+"""Cache, attention, residual norm without a GPU: sizes, and every refusal before any CUDA call (the pointers are fakes that
+are never followed)."""
+import ctypes
+
+import pytest
+
+import paper_2402_15319_b200 as vq
+from paper_2402_15319_b200 import binding, build as vq_build
+from tests.kv_ref import Books
+
+FAKE, ODD, ODD4 = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10008), ctypes.c_void_p(0x10002)
+GOOD = vq.VQKVFormat(32, 16, 4, 128, vq.VQ_KV_FP16)
+OK, NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED = 0, 1, 2, 3, 4, 5, 7
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    vq_build.build()
+
+
+def _fmt(**kw):
+    return vq.VQKVFormat(**{**GOOD.__dict__, **kw})
+
+
+def _pool(fmt, **kw):
+    i8 = fmt.kv_type == vq.VQ_KV_INT8
+    f = dict(d_k=FAKE, d_v=FAKE, d_k_scale=FAKE if i8 else None, d_v_scale=FAKE if i8 else None)
+    return binding._CKVPool(**{**f, **kw})
+
+
+def _seqs(**kw):
+    return binding._CKVSeqs(**{**dict(d_table=FAKE, d_len=FAKE, n_seqs=3, table_stride=8), **kw})
+
+
+def test_sizes():
+    i = vq.vq_kv_info(GOOD)
+    assert i.pool_bytes == 32 * 4 * 16 * 128 * 2 and i.scale_bytes == 0 and i.page_bytes == 2 * 4 * 16 * 256
+    i = vq.vq_kv_info(_fmt(kv_type=vq.VQ_KV_INT8, head_dim=80))
+    assert i.pool_bytes == 32 * 4 * 16 * 80 and i.scale_bytes == 32 * 4 * 16 * 4 and i.page_bytes == 2 * 4 * 16 * 84
+    assert vq.vq_kv_info(_fmt(n_pages=1 << 20)).pool_bytes == (1 << 20) * 4 * 16 * 256   # beyond 32 bits
+    assert vq.vq_kv_attention_workspace_bytes(GOOD) > 0
+    assert vq.vq_kv_attention_workspace_bytes(_fmt(head_dim=48)) == 0     # no kernel for it
+    assert vq.vq_kv_pages_workspace_bytes(GOOD, 5) > 0 and vq.vq_kv_pages_workspace_bytes(GOOD, 0) == 0
+    assert vq.vq_kv_pages_workspace_bytes(_fmt(n_pages=100), 7) > vq.vq_kv_pages_workspace_bytes(_fmt(n_pages=10), 7)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(kv_type=2), FORMAT), (dict(kv_type=-1), FORMAT), (dict(page_tokens=4), FORMAT), (dict(page_tokens=24), FORMAT), (dict(page_tokens=512), FORMAT),
+    (dict(page_tokens=0), FORMAT), (dict(head_dim=0), FORMAT), (dict(head_dim=72), FORMAT), (dict(head_dim=272), FORMAT), (dict(head_dim=-16), FORMAT),
+    (dict(n_pages=0), SHAPE), (dict(n_kv_heads=0), SHAPE), (dict(n_kv_heads=-3), SHAPE),
+])
+def test_bad_formats(kw, code):
+    f = _fmt(**kw)
+    with pytest.raises(vq.VQError) as e:
+        vq.vq_kv_info(f)
+    assert e.value.code == code
+    assert vq.vq_kv_attention_workspace_bytes(f) == 0 and vq.vq_kv_pages_workspace_bytes(f, 3) == 0
+    assert _attend(f) == code and _append(f) == code and _reserve(f) == code and _fork(f) == code and _compact(f) == code
+    assert _free(f) == code and _copy(f) == code
+
+
+def _attend(fmt=GOOD, pool=None, seqs=None, hq=8, q=FAKE, qs=1024, out=FAKE, os=1024, lse=None, window=0, ws=FAKE, ws_bytes=1 << 30):
+    pool, seqs, c = pool or _pool(fmt), seqs or _seqs(), fmt.c()
+    return vq.load().vq_kv_attention(ctypes.byref(c), ctypes.byref(pool), ctypes.byref(seqs), hq, q, qs, out, os, lse, 0.1, window, ws, ws_bytes, None)
+
+
+def test_attention_refusals():
+    i8 = _fmt(kv_type=vq.VQ_KV_INT8)
+    for kw in (dict(d_k=None), dict(d_v=None), dict(d_k_scale=FAKE), dict(d_v_scale=FAKE)):
+        assert _attend(pool=_pool(GOOD, **kw)) == NULL
+    assert _attend(i8, pool=_pool(i8, d_k_scale=None)) == NULL
+    assert _attend(pool=_pool(GOOD, d_k=ODD)) == ALIGN and _attend(i8, pool=_pool(i8, d_v_scale=ODD)) == ALIGN
+    assert _attend(seqs=_seqs(d_table=None)) == NULL and _attend(seqs=_seqs(d_len=None)) == NULL
+    assert _attend(seqs=_seqs(d_len=ODD4)) == ALIGN
+    for kw in (dict(n_seqs=0), dict(n_seqs=65537), dict(table_stride=0), dict(table_stride=-1), dict(table_stride=(1 << 26) + 1)):
+        assert _attend(seqs=_seqs(**kw)) == SHAPE
+    assert _attend(q=None) == NULL and _attend(out=None) == NULL
+    assert _attend(q=ODD) == ALIGN and _attend(out=ODD) == ALIGN and _attend(lse=ODD4) == ALIGN and _attend(ws=ODD) == ALIGN
+    assert _attend(hq=0) == SHAPE and _attend(hq=6) == SHAPE and _attend(hq=-4) == SHAPE and _attend(window=-1) == SHAPE
+    assert _attend(qs=1023) == SHAPE and _attend(os=1000) == SHAPE and _attend(qs=1028) == ALIGN and _attend(os=1025) == ALIGN
+    assert _attend(ws=None) == WORKSPACE and _attend(ws_bytes=vq.vq_kv_attention_workspace_bytes(GOOD) - 1) == WORKSPACE
+    assert _attend(_fmt(head_dim=48)) == UNSUPPORTED
+
+
+def _append(fmt=GOOD, pool=None, seqs=None, starts=None, n=3, k=FAKE, ks=512, v=FAKE, vs=512, rot=None):
+    pool, seqs, c = pool or _pool(fmt), seqs or _seqs(), fmt.c()
+    return vq.load().vq_kv_append(ctypes.byref(c), ctypes.byref(pool), ctypes.byref(seqs), starts, n, k, ks, v, vs,
+                                  None if rot is None else ctypes.byref(rot), None)
+
+
+def _rot(**kw):
+    f = dict(d_cos_sin=FAKE, n_positions=128, rot_dim=128, interleaved=0, n_q_heads=8, d_q=FAKE, d_q_out=FAKE, q_stride=1024, q_out_stride=1024)
+    return binding._CKVRotary(**{**f, **kw})
+
+
+def test_append_refusals():
+    assert _append(k=None) == NULL and _append(v=None) == NULL and _append(pool=_pool(GOOD, d_v=None)) == NULL
+    assert _append(n=2) == SHAPE and _append(n=0, starts=FAKE) == SHAPE and _append(ks=511) == SHAPE and _append(vs=500) == SHAPE
+    assert _append(ks=516) == ALIGN and _append(k=ODD) == ALIGN and _append(v=ODD) == ALIGN and _append(starts=ODD4) == ALIGN
+    assert _append(rot=_rot(d_cos_sin=None)) == NULL and _append(rot=_rot(d_q=None)) == NULL and _append(rot=_rot(d_q_out=None)) == NULL
+    assert _append(rot=_rot(n_q_heads=0)) == NULL         # queries without heads
+    for kw in (dict(rot_dim=8), dict(rot_dim=144), dict(rot_dim=24), dict(n_q_heads=-1), dict(n_positions=127), dict(interleaved=2), dict(q_stride=1016),
+               dict(q_out_stride=8), dict(q_stride=1032)):
+        assert _append(rot=_rot(**kw)) == SHAPE, kw       # (the last: in place, with another stride)
+    assert _append(rot=_rot(d_cos_sin=ODD)) == ALIGN and _append(rot=_rot(d_q=ODD)) == ALIGN and _append(rot=_rot(q_stride=1028)) == ALIGN
+
+
+def _reserve(fmt=GOOD, seqs=None, refs=FAKE, new=None, status=FAKE, ws=FAKE, ws_bytes=1 << 30):
+    seqs, c = seqs or _seqs(), fmt.c()
+    return vq.load().vq_kv_reserve(ctypes.byref(c), ctypes.byref(seqs), refs, new, status, ws, ws_bytes, None)
+
+
+def _fork(fmt=GOOD, n_layers=2, seqs=None, refs=FAKE, pairs=FAKE, n=2, status=FAKE, ws=FAKE, ws_bytes=1 << 30, pools=True):
+    seqs, c = seqs or _seqs(), fmt.c()
+    arr = (binding._CKVPool * 121)(*[_pool(fmt)] * 121) if pools else None
+    return vq.load().vq_kv_fork(ctypes.byref(c), arr, n_layers, ctypes.byref(seqs), refs, pairs, n, status, ws, ws_bytes, None)
+
+
+def _compact(fmt=GOOD, n_layers=2, seqs=None, refs=FAKE, status=FAKE, ws=FAKE, ws_bytes=1 << 30, pools=True):
+    seqs, c = seqs or _seqs(), fmt.c()
+    arr = (binding._CKVPool * 121)(*[_pool(fmt)] * 121) if pools else None
+    return vq.load().vq_kv_compact(ctypes.byref(c), arr, n_layers, ctypes.byref(seqs), refs, status, ws, ws_bytes, None)
+
+
+def _copy(fmt=GOOD, n_layers=2, pairs=FAKE, n=2, pools=True):
+    c = fmt.c()
+    arr = (binding._CKVPool * 121)(*[_pool(fmt)] * 121) if pools else None
+    return vq.load().vq_kv_copy_pages(ctypes.byref(c), arr, n_layers, pairs, n, None)
+
+
+def _free(fmt=GOOD, seqs=None, refs=FAKE, slots=FAKE, n=2):
+    seqs, c = seqs or _seqs(), fmt.c()
+    return vq.load().vq_kv_free(ctypes.byref(c), ctypes.byref(seqs), refs, slots, n, None)
+
+
+def test_page_refusals():
+    need = vq.vq_kv_pages_workspace_bytes(GOOD, 3)
+    for call in (_reserve, _fork, _compact):
+        assert call(refs=None) == NULL and call(status=None) == NULL and call(refs=ODD4) == ALIGN and call(status=ODD4) == ALIGN
+        assert call(ws=None) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE and call(ws=ODD) == ALIGN
+        assert call(seqs=_seqs(n_seqs=0)) == SHAPE and call(seqs=_seqs(d_len=None)) == NULL
+    assert _reserve(new=ODD4) == ALIGN
+    for call in (_fork, _compact, _copy):
+        assert call(pools=False) == NULL and call(n_layers=0) == SHAPE and call(n_layers=121) == SHAPE
+    assert _fork(pairs=None) == NULL and _fork(n=0) == SHAPE and _fork(n=1025) == SHAPE and _fork(pairs=ODD4) == ALIGN
+    assert _copy(pairs=None) == NULL and _copy(n=0) == SHAPE and _copy(n=(1 << 24) + 1) == SHAPE and _copy(pairs=ODD4) == ALIGN
+    assert _free(slots=None) == NULL and _free(refs=None) == NULL and _free(n=0) == SHAPE and _free(n=65537) == SHAPE and _free(slots=ODD4) == ALIGN
+
+
+NORM = vq.VQNorm(4, 64, vq.VQ_NORM_RMS, vq.VQ_RESIDUAL_FP16, vq.VQ_GATE_NONE, 1e-5, 1.0, 64, 64, 64, 64, 64)
+
+
+def _norm(x=FAKE, y=FAKE, gate=None, post_w=None, post_b=None, pre_w=FAKE, pre_b=None, x_out=FAKE, h=FAKE, **kw):
+    c = vq.VQNorm(**{**NORM.__dict__, **kw}).c()
+    return vq.load().vq_residual_norm(ctypes.byref(c), x, y, gate, post_w, post_b, pre_w, pre_b, x_out, h, None)
+
+
+def test_norm_refusals():
+    other = ctypes.c_void_p(0x20000)
+    assert vq.load().vq_residual_norm(None, *[FAKE] * 9, None) == NULL
+    assert _norm(x=None) == NULL and _norm(x_out=None, h=None, pre_w=None) == NULL
+    assert _norm(pre_w=None) == NULL and _norm(h=None) == NULL                # a norm and its output come together
+    assert _norm(gate=FAKE) == NULL                                           # a gate that the block does not name
+    assert _norm(post_b=FAKE) == NULL and _norm(h=None, pre_w=None, pre_b=FAKE) == NULL
+    assert _norm(y=None, post_w=FAKE) == NULL and _norm(y=None, post_w=FAKE, post_b=FAKE) == NULL
+    c = vq.VQNorm(**{**NORM.__dict__, "gate": vq.VQ_GATE_CHANNEL}).c()
+    assert vq.load().vq_residual_norm(ctypes.byref(c), FAKE, FAKE, None, None, None, FAKE, None, FAKE, other, None) == NULL
+    for kw in (dict(kind=2), dict(kind=-1), dict(residual_type=2)):
+        assert _norm(**kw) == FORMAT
+    c = vq.VQNorm(**{**NORM.__dict__, "gate": 3}).c()
+    assert vq.load().vq_residual_norm(ctypes.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, None, FAKE, other, None) == FORMAT
+    for kw in (dict(n_rows=0), dict(n_cols=0), dict(n_cols=32769), dict(n_cols=65), dict(x_stride=63), dict(y_stride=63), dict(x_out_stride=63),
+               dict(h_stride=63)):
+        assert _norm(h=other, **kw) == SHAPE, kw
+    assert _norm(h=other, x_out_stride=72) == SHAPE and _norm(h=FAKE, h_stride=72, x_out=other) == SHAPE   # in place with another stride
+    for name in ("x", "y", "pre_w", "x_out", "h", "pre_b"):
+        assert _norm(**{"h": other, **{name: ODD}}) == ALIGN
+    assert _norm(h=other, post_w=ODD) == ALIGN
+
+
+def test_host_tensors_are_refused():
+    torch = pytest.importorskip("torch")
+    t = torch.zeros(8, 8, dtype=torch.int32)
+    with pytest.raises(ValueError, match="current device"):
+        vq.vq_kv_reserve(GOOD, vq.KVSeqs(t, t[0].contiguous()), t, None, t, t)
+    with pytest.raises(ValueError, match="current device"):
+        vq.vq_residual_norm(NORM, t, t, None, None, None, t, None, t, t)
+
+
+def test_books_follow_the_rules():
+    """The model that the GPU tests compare with, on a case worked out by hand."""
+    b = Books(8, 8, 4, 4)
+    assert b.reserve([17, 0, 8, 0]) == (0, 0)
+    assert b.table[0][:3] == [0, 1, 2] and b.table[2][:1] == [3] and b.len == [17, 0, 8, 0]
+    assert b.reserve([0, 0, 0, 33]) == (0, 1)                    # five pages, a row has four
+    assert b.reserve([9, 30, 0, 0]) == (1, 0)                    # 1 + 4 pages, four are free
+    status, copies = b.fork([(0, 1), (0, 1), (2, 3), (9, 3), (0, 2)])
+    assert status == (0, 3) and copies == [(2, 4, 1)]            # page 2 has one token
+    assert b.table[1][:3] == [0, 1, 4] and b.table[3][0] == 3 and b.refs == [2, 2, 1, 2, 1, 0, 0, 0] and b.len == [17, 17, 8, 8]
+    b.free([0, 0, 7])
+    assert b.refs == [1, 1, 0, 2, 1, 0, 0, 0] and b.len[0] == 0
+    status, copies = b.compact()
+    assert status == (4, 1) and copies == [(4, 2, 8)] and b.table[1][:3] == [0, 1, 2] and b.refs == [1, 1, 1, 2, 0, 0, 0, 0]
