@@ -11,7 +11,7 @@ from .binding import (  # noqa: F401
     vq_int4g128_gemm_small_batch, vq_int4g128_workspace_bytes, vq_status_string, vq_device_wait_failures,
     vq_assign_indices, vq_unpack_uniform, vq_probe_decode_loop, vq_probe_read, VQ_UNPACK_FP16, VQ_UNPACK_INT8_ROW, VQ_UNPACK_INT4_G128,
     VQ_KV_FP16, VQ_KV_INT8, VQ_KV_MAX_LAYERS, VQ_NORM_RMS, VQ_NORM_LAYER, VQ_RESIDUAL_FP16, VQ_RESIDUAL_FP32,
-    VQ_GATE_NONE, VQ_GATE_CHANNEL, VQ_GATE_ELEMENT, VQKVFormat, KVInfo, KVPool, KVSeqs, KVRotary, VQNorm,
+    VQ_GATE_NONE, VQ_GATE_CHANNEL, VQ_GATE_ELEMENT, VQKVFormat, KVInfo, KVPool, KVPools, KVSeqs, KVRotary, VQNorm,
     vq_kv_info, vq_kv_attention, vq_kv_attention_workspace_bytes, vq_kv_append, vq_kv_pages_workspace_bytes, vq_kv_reserve, vq_kv_fork,
     vq_kv_free, vq_kv_compact, vq_kv_copy_pages, vq_residual_norm,
 )

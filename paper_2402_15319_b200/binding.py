@@ -7,7 +7,6 @@ import ctypes
 import functools
 import os
 from dataclasses import dataclass
-from typing import NamedTuple
 
 VQ_CB_FP16, VQ_CB_INT8_SCALED, VQ_CB_INT4_G128 = 0, 1, 2
 VQ_IMPL_AUTO, VQ_IMPL_GENERIC, VQ_IMPL_TUNED, VQ_IMPL_STREAM, VQ_IMPL_TILE = 0, 1, 2, 3, 4
@@ -385,21 +384,30 @@ class _CNormBlock(ctypes.Structure):
                 [(n, ctypes.c_int64) for n in ("x_stride", "y_stride", "gate_stride", "x_out_stride", "h_stride")])
 
 
+# Formats and handles hold their C struct (the library only reads it): a call passes its address.
+
+class _Held:
+    __slots__ = ("_c", "_p", "device")   # (not among the fields)
+
+    def _hold(self, struct, device=None) -> None:
+        object.__setattr__(self, "_c", struct)
+        object.__setattr__(self, "_p", ctypes.addressof(struct))
+        object.__setattr__(self, "device", device)
+
+
 @dataclass(frozen=True)
-class VQKVFormat:
+class VQKVFormat(_Held):
     n_pages: int
     page_tokens: int
     n_kv_heads: int
     head_dim: int
     kv_type: int
 
+    def __post_init__(self):
+        self._hold(_CKVFormat(self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.kv_type))
+
     def c(self) -> _CKVFormat:
-        return _c_kv_format(self)
-
-
-@functools.lru_cache(maxsize=4096)
-def _c_kv_format(f: "VQKVFormat") -> _CKVFormat:
-    return _CKVFormat(f.n_pages, f.page_tokens, f.n_kv_heads, f.head_dim, f.kv_type)
+        return self._c
 
 
 @dataclass(frozen=True)
@@ -409,22 +417,46 @@ class KVInfo:
     page_bytes: int
 
 
-class KVPool(NamedTuple):
-    """One layer's pool: keys and values, and their scales for VQ_KV_INT8."""
+def _device_of(*tensors):
+    """Device index that all tensors share (-1: the host; None without tensors)."""
+    devices = {t.get_device() for t in tensors if t is not None} or {None}
+    if len(devices) != 1:
+        raise ValueError(f"tensors on different devices: {sorted(devices)}")
+    return devices.pop()
+
+
+@dataclass(frozen=True, eq=False)
+class KVPool(_Held):
+    """One layer's pool: keys and values, and their scales for VQ_KV_INT8.  Holds the tensors; their memory has to stay where
+    it is while the handle is used."""
     k: object
     v: object
     k_scale: object = None
     v_scale: object = None
 
+    def __post_init__(self):
+        self._hold(_CKVPool(*[_ptr(t) for t in self]), _device_of(*self))
 
-class KVSeqs(NamedTuple):
-    """Page table (int32, a row per sequence) and lengths (int32)."""
+    def __iter__(self):
+        return iter((self.k, self.v, self.k_scale, self.v_scale))
+
+
+@dataclass(frozen=True, eq=False)
+class KVSeqs(_Held):
+    """Page table (int32, a row per sequence) and lengths (int32).  Holds the tensors, as KVPool does."""
     table: object
     length: object
 
+    def __post_init__(self):
+        table, length = self.table, self.length
+        if table.dim() != 2 or not table.is_contiguous() or length.dim() != 1 or not length.is_contiguous() or length.shape[0] != table.shape[0]:
+            raise ValueError("KVSeqs: a contiguous table, and a length for each of its rows")
+        self._hold(_CKVSeqs(table.data_ptr(), length.data_ptr(), table.shape[0], table.shape[1]), _device_of(table, length))
 
-class KVRotary(NamedTuple):
-    """Cosines and sines, and the new tokens' queries (None: keys only)."""
+
+@dataclass(frozen=True, eq=False)
+class KVRotary(_Held):
+    """Cosines and sines, and the new tokens' queries (None: keys only).  Holds the tensors, as KVPool does."""
     d_cos_sin: object
     n_positions: int
     rot_dim: int
@@ -435,9 +467,14 @@ class KVRotary(NamedTuple):
     d_q_out: object = None
     q_out_stride: int = 0
 
+    def __post_init__(self):
+        self._hold(_CKVRotary(_ptr(self.d_cos_sin), int(self.n_positions), int(self.rot_dim), int(self.interleaved), int(self.n_q_heads),
+                              _ptr(self.d_q), _ptr(self.d_q_out), int(self.q_stride), int(self.q_out_stride)),
+                   _device_of(self.d_cos_sin, self.d_q, self.d_q_out))
+
 
 @dataclass(frozen=True)
-class VQNorm:
+class VQNorm(_Held):
     n_rows: int
     n_cols: int
     kind: int
@@ -451,46 +488,59 @@ class VQNorm:
     x_out_stride: int = 0
     h_stride: int = 0
 
+    def __post_init__(self):
+        self._hold(_CNormBlock(self.n_rows, self.n_cols, self.kind, self.residual_type, self.gate, self.eps, self.residual_scale, self.x_stride,
+                               self.y_stride, self.gate_stride, self.x_out_stride, self.h_stride))
+
     def c(self) -> _CNormBlock:
-        return _c_norm(self)
+        return self._c
 
 
-@functools.lru_cache(maxsize=4096)
-def _c_norm(n: "VQNorm") -> _CNormBlock:
-    return _CNormBlock(n.n_rows, n.n_cols, n.kind, n.residual_type, n.gate, n.eps, n.residual_scale, n.x_stride, n.y_stride, n.gate_stride,
-                       n.x_out_stride, n.h_stride)
+class KVPools:
+    """The pools of a cache's layers, in order (a list of KVPool does as well: it is laid out at every call)."""
+
+    def __init__(self, pools):
+        self.pools = tuple(pools)
+        devices = {p.device for p in self.pools}
+        if len(devices) > 1:
+            raise ValueError(f"pools on different devices: {sorted(devices)}")
+        self.device = devices.pop() if devices else None
+        self._c = (_CKVPool * len(self.pools))(*[p._c for p in self.pools])
+        self._p = ctypes.addressof(self._c)
+
+
+def _pools(pools) -> KVPools:
+    return pools if isinstance(pools, KVPools) else KVPools(pools)
 
 
 _current_device = None
 
 
-def _here(*tensors) -> None:
-    """The calls below launch on the current device: a tensor of another one (or of the host) is refused."""
+def _device_now() -> int:
     global _current_device
     if _current_device is None:
         import torch
         _current_device = torch.cuda.current_device if torch.cuda.is_available() else lambda: 0
-    dev = _current_device()
+    return _current_device()
+
+
+def _elsewhere(now, *operands):
+    for t in operands:
+        if t is not None:
+            dev = t.get_device() if hasattr(t, "get_device") else t.device
+            if dev is not None and dev != now:
+                raise ValueError(f"operand on device {dev}, the current device is cuda:{now}")
+
+
+def _here(handles, *tensors) -> None:
+    """The calls below launch on the current device: operands of another one (or of the host) are refused."""
+    now = _device_now()
+    for h in handles:
+        if h.device != now:
+            _elsewhere(now, *handles)
     for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
-
-
-def _c_pool(pool: KVPool) -> _CKVPool:
-    _here(*pool)
-    return _CKVPool(*[_ptr(t) for t in pool])
-
-
-def _c_pools(pools):
-    return (_CKVPool * len(pools))(*[_c_pool(p) for p in pools])
-
-
-def _c_seqs(seqs: KVSeqs) -> _CKVSeqs:
-    table, length = seqs
-    _here(table, length)
-    if table.dim() != 2 or not table.is_contiguous() or length.dim() != 1 or not length.is_contiguous() or length.shape[0] != table.shape[0]:
-        raise ValueError("KVSeqs: a contiguous table, and a length for each of its rows")
-    return _CKVSeqs(table.data_ptr(), length.data_ptr(), table.shape[0], table.shape[1])
+        if t is not None and t.get_device() != now:
+            _elsewhere(now, t)
 
 
 def _bytes(t) -> int:
@@ -499,75 +549,70 @@ def _bytes(t) -> int:
 
 def vq_kv_info(fmt: VQKVFormat) -> KVInfo:
     out = _CKVInfo()
-    _check(load().vq_kv_info(ctypes.byref(fmt.c()), ctypes.byref(out)), "vq_kv_info")
+    _check(load().vq_kv_info(fmt._p, ctypes.byref(out)), "vq_kv_info")
     return KVInfo(int(out.pool_bytes), int(out.scale_bytes), int(out.page_bytes))
 
 
 def vq_kv_attention_workspace_bytes(fmt: VQKVFormat) -> int:
-    return load().vq_kv_attention_workspace_bytes(ctypes.byref(fmt.c()))
+    return load().vq_kv_attention_workspace_bytes(fmt._p)
 
 
 def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int, d_q, q_stride: int, d_out, out_stride: int, d_lse, scale: float,
                     window: int, d_ws, stream=None) -> None:
     """One new token per sequence over the paged cache; window 0: all of it.  d_lse may be None."""
-    _here(d_q, d_out, d_lse, d_ws)
-    _check(load().vq_kv_attention(ctypes.byref(fmt.c()), ctypes.byref(_c_pool(pool)), ctypes.byref(_c_seqs(seqs)), int(n_q_heads), _ptr(d_q),
-                                  int(q_stride), _ptr(d_out), int(out_stride), _ptr(d_lse), float(scale), int(window), _ptr(d_ws), _bytes(d_ws),
-                                  _stream(stream)), "vq_kv_attention")
+    _here((pool, seqs), d_q, d_out, d_lse, d_ws)
+    _check(load().vq_kv_attention(fmt._p, pool._p, seqs._p, n_q_heads, _ptr(d_q), q_stride, _ptr(d_out), out_stride, _ptr(d_lse), scale,
+                                  window, d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_attention")
 
 
 def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens: int, d_k, k_stride: int, d_v, v_stride: int,
                  rotary: KVRotary | None = None, stream=None) -> None:
     """New tokens into the cache.  d_starts None: one token per sequence."""
-    _here(d_starts, d_k, d_v)
-    r = None
-    if rotary is not None:
-        _here(rotary.d_cos_sin, rotary.d_q, rotary.d_q_out)
-        r = ctypes.byref(_CKVRotary(_ptr(rotary.d_cos_sin), int(rotary.n_positions), int(rotary.rot_dim), int(rotary.interleaved),
-                                    int(rotary.n_q_heads), _ptr(rotary.d_q), _ptr(rotary.d_q_out), int(rotary.q_stride), int(rotary.q_out_stride)))
-    _check(load().vq_kv_append(ctypes.byref(fmt.c()), ctypes.byref(_c_pool(pool)), ctypes.byref(_c_seqs(seqs)), _ptr(d_starts), int(n_tokens),
-                               _ptr(d_k), int(k_stride), _ptr(d_v), int(v_stride), r, _stream(stream)), "vq_kv_append")
+    _here((pool, seqs) if rotary is None else (pool, seqs, rotary), d_starts, d_k, d_v)
+    _check(load().vq_kv_append(fmt._p, pool._p, seqs._p, _ptr(d_starts), n_tokens, _ptr(d_k), k_stride, _ptr(d_v), v_stride,
+                               None if rotary is None else rotary._p, _stream(stream)), "vq_kv_append")
 
 
 def vq_kv_pages_workspace_bytes(fmt: VQKVFormat, n_seqs: int) -> int:
-    return load().vq_kv_pages_workspace_bytes(ctypes.byref(fmt.c()), int(n_seqs))
+    return load().vq_kv_pages_workspace_bytes(fmt._p, n_seqs)
 
 
 def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, stream=None) -> None:
     """Room for d_new tokens per sequence (None: one each); d_status: pages missing, sequences too long."""
-    _here(d_refs, d_new, d_status, d_ws)
-    _check(load().vq_kv_reserve(ctypes.byref(fmt.c()), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_new), _ptr(d_status), _ptr(d_ws),
-                                _bytes(d_ws), _stream(stream)), "vq_kv_reserve")
+    _here((seqs,), d_refs, d_new, d_status, d_ws)
+    _check(load().vq_kv_reserve(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_new), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
+                                _stream(stream)), "vq_kv_reserve")
 
 
 def vq_kv_fork(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_pairs, n_pairs: int, d_status, d_ws, stream=None) -> None:
-    """pools: one KVPool per layer.  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
-    _here(d_refs, d_pairs, d_status, d_ws)
-    _check(load().vq_kv_fork(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_pairs),
-                             int(n_pairs), _ptr(d_status), _ptr(d_ws), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
+    """pools: a KVPool per layer (KVPools).  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
+    pools = _pools(pools)
+    _here((pools, seqs), d_refs, d_pairs, d_status, d_ws)
+    _check(load().vq_kv_fork(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_pairs), n_pairs, _ptr(d_status),
+                             d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
 
 
 def vq_kv_free(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_slots, n_slots: int, stream=None) -> None:
-    _here(d_refs, d_slots)
-    _check(load().vq_kv_free(ctypes.byref(fmt.c()), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_slots), int(n_slots), _stream(stream)),
-           "vq_kv_free")
+    _here((seqs,), d_refs, d_slots)
+    _check(load().vq_kv_free(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_slots), n_slots, _stream(stream)), "vq_kv_free")
 
 
 def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, stream=None) -> None:
     """d_status: pages in use, pages moved."""
-    _here(d_refs, d_status, d_ws)
-    _check(load().vq_kv_compact(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), ctypes.byref(_c_seqs(seqs)), _ptr(d_refs), _ptr(d_status),
-                                _ptr(d_ws), _bytes(d_ws), _stream(stream)), "vq_kv_compact")
+    pools = _pools(pools)
+    _here((pools, seqs), d_refs, d_status, d_ws)
+    _check(load().vq_kv_compact(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
+                                _stream(stream)), "vq_kv_compact")
 
 
 def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None) -> None:
-    _here(d_pairs)
-    _check(load().vq_kv_copy_pages(ctypes.byref(fmt.c()), _c_pools(pools), len(pools), _ptr(d_pairs), int(n_pairs), _stream(stream)),
-           "vq_kv_copy_pages")
+    pools = _pools(pools)
+    _here((pools,), d_pairs)
+    _check(load().vq_kv_copy_pages(fmt._p, pools._p, len(pools.pools), _ptr(d_pairs), n_pairs, _stream(stream)), "vq_kv_copy_pages")
 
 
 def vq_residual_norm(norm: VQNorm, d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h, stream=None) -> None:
     """x' = x + residual_scale * gate * post(y), h = pre(x'); absent operands are None."""
-    operands = (d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h)
-    _here(*operands)
-    _check(load().vq_residual_norm(ctypes.byref(norm.c()), *[_ptr(t) for t in operands], _stream(stream)), "vq_residual_norm")
+    _here((), d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h)
+    _check(load().vq_residual_norm(norm._p, _ptr(d_x), _ptr(d_y), _ptr(d_gate), _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b),
+                                   _ptr(d_x_out), _ptr(d_h), _stream(stream)), "vq_residual_norm")

@@ -1,18 +1,21 @@
 // Attention of one new token per sequence over a paged cache (vq_kv_attention).
 //
 //   out[h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q_h . k_t - m),  m the running maximum,
-// one pass over keys and values (the softmax's maximum and sum run along, accumulators are rescaled when the maximum grows).
+// one pass over keys and values: maximum and sum run along, accumulators are rescaled when the maximum has grown by a factor
+// of 2^kSlack (weights stay in range till then, so most tiles need no exchange between lanes).
 //
 // Bound by memory: every key and value is read once, 4 * group multiply-adds per pair of stored values, far below what the
-// tensor cores need (8 query heads per key/value head at 6.5 TB/s are 0.1 PFLOP/s with the 16-row tile padded).  So the
-// products run as mma.sync on 16 x 16 x 8 tiles, the query heads of one key/value head as the rows: no operand passes
-// through tensor memory, and the scores stay in the registers that the second product reads.
+// tensor cores need.  So the products run as mma.sync m16n8k16 straight from the tiles in shared memory, the tokens (first
+// product) and the dimensions (second) as the 16 rows, eight query heads of one key/value head as the columns: no operand
+// passes through tensor memory, and the scores turn into the second product's operand in registers (movmatrix).
 //
 // Split: the tokens of all sequences and key/value heads form one list of tiles (sequence, head, tile); each CTA takes an
-// equal run of it, wherever sequences end, so lengths need not be known on the host and ragged batches stay balanced.
-// Inside a CTA the warps take tiles in turn, each with its own ring of asynchronous copies: no barrier inside a run.
-// A head whose run of tiles is cut between CTAs leaves partial sums (accumulators, maximum, sum) in the workspace; the CTA
-// that arrives last joins them in the order of the CTAs, so results do not depend on which one that is.
+// equal run of it and each warp an equal part of that, wherever sequences end, so lengths need not be known on the host
+// and ragged batches stay balanced.  A warp has a ring of tiled TMA copies of its own (a box never crosses a page; lane i
+// requests box i, so a tile costs the warp one request) that runs on over the ends of sequences: there is no barrier
+// before the end of the run.  A head that lies in one warp's part is finished there.  What is cut between warps is joined
+// at the CTA's end, what is cut between CTAs goes to the workspace (accumulators, maximum, sum) and is joined by the CTA
+// that arrives last - in the order of the list, so results do not depend on which one that is.
 #include <math.h>
 
 #include "vq_device.cuh"
@@ -23,16 +26,16 @@ namespace {
 
 using namespace dev;
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kMaxCtas = 512;           // CTAs of a launch (partial sums and counters are sized for them)
-constexpr int kChunkRows = 16;          // query heads that a CTA takes together
-// p is held as 2^kLift * exp(...): binary16 pieces of small weights stay normal down to 2^-28 of the largest weight.
-constexpr float kLift = 14.0f;
+constexpr int kToll = 2;                // places in front of a head's tiles: what beginning and ending one costs, in tiles
+constexpr int kWaitTries = 1 << 18;     // mbarrier polls before a warp gives up and flags an error
+constexpr int kMaxHeads = 16;           // query heads that a CTA takes together at most
+constexpr int kMaxCtas = 256;          // CTAs of a launch, one per SM (partial sums and counters are sized for them)
+constexpr int kMaxWarps = 8;
+// Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, and two binary16 pieces hold a weight of
+// 2^-18 of the largest to 2^-32 of it.
+constexpr float kLift = 7.0f, kSlack = 8.0f;
 
 struct AttnArgs {
-  const uint8_t* k;
-  const uint8_t* v;
   const float* ks;
   const float* vs;
   const int* table;
@@ -42,8 +45,9 @@ struct AttnArgs {
   float* lse;
   float* partial;
   int* counters;
+  int* error_flag;
   long long q_stride, out_stride;
-  int n_seqs, table_stride, max_len, n_pages, page_shift, heads, group, chunks, n_q_heads, window;
+  int n_seqs, table_stride, max_len, n_pages, page_shift, run_shift, heads, group, chunks, n_q_heads, window;
   float scale_log2;
 };
 
@@ -52,27 +56,41 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Counts an arrival; what the CTA wrote (in front of its barrier) is there for whoever counts later.
+__device__ __forceinline__ int arrive(int* counter) {
+  int old;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+  return old;
+}
+__device__ __forceinline__ float lds_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ float log2_fast(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
-  const int bytes = on ? 16 : 0;   // 0: zeros, nothing is read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+// Transposes an 8 x 8 matrix of binary16 held a row to four lanes.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f; }   // 0: no token at all
+__device__ __forceinline__ float log_sum(float top, float sum) {   // natural, of 2^(top - kLift) * sum
+  return ((top == -INFINITY ? 0.0f : top) - kLift + log2f(sum)) * 0.693147180559945309f;
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 // Two signed bytes (already offset by 128) into binary16, exactly: 0x6400 | u is 1024 + u.
@@ -85,504 +103,881 @@ __device__ __forceinline__ uint32_t bytes_to_half2(uint32_t u) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
-// Shapes of one instantiation.
-template <int D, bool I8>
+// Shapes of one instantiation: head dimension, 8-bit cache, groups of eight query heads taken together.
+template <int D, bool I8, int NH>
 struct Shape {
   static constexpr int ROW = D * (I8 ? 1 : 2);          // bytes of one token
-  static constexpr int CH = ROW / 16;                   // 16-byte pieces of one token
-  static constexpr int PITCH = (CH | 1) * 16;           // odd in pieces: eight rows of a matrix lie in different banks
+  // A tile lies in shared memory as column blocks of 128 bytes (64 where a row has no more) by tokens, 16-byte pieces
+  // swizzled by the copy: eight rows of a matrix lie in different banks.  Columns beyond the row are filled, not read.
+  static constexpr int CBB = ROW <= 64 ? 64 : 128;
+  static constexpr int NCB = (ROW + CBB - 1) / CBB;
   // tokens per tile: a stage of a warp holds about 8 KB of keys and values
   static constexpr int R = I8 ? (ROW <= 64 ? 4 : 2) : (ROW <= 128 ? 2 : 1);
   static constexpr int TT = 16 * R;
   static constexpr int HALVES = TT / 8;                 // runs of 8 tokens: never across a page
-  static constexpr int KV = TT * PITCH;
-  static constexpr int STAGE = 2 * KV + (I8 ? 2 * TT * 4 : 0);
-  static constexpr int CTAS = 3 * kWarps * STAGE + 2048 <= 113 * 1024 ? 2 : 1;   // resident per SM
-  static constexpr int FIT = ((CTAS == 2 ? 113 : 226) * 1024 - 2048) / (kWarps * STAGE);
-  static constexpr int NS = FIT > 6 ? 6 : FIT;          // stages of a warp's ring
-  static constexpr size_t JOIN = static_cast<size_t>(kWarps) * kChunkRows * (D + 2) * 4;   // (reuses the rings)
-  static constexpr size_t SMEM = static_cast<size_t>(kWarps) * NS * STAGE > JOIN ? static_cast<size_t>(kWarps) * NS * STAGE : JOIN;
-  static_assert(NS >= 2, "a ring needs two stages");
+  static constexpr int WIN = 32 / HALVES;               // tiles whose pages a warp's lanes hold
+  static constexpr int KV = TT * NCB * CBB;
+  static constexpr int STAGE = 2 * KV;
+  static constexpr int SCALES = I8 ? 2 * TT * 4 : 0;    // per stage, behind the rings
+  static constexpr int HEADS = 8 * NH;
+  static constexpr int JROW = D + 4;                    // a row of the join's sums: heads of a lane's neighbours in different banks
+  static constexpr int SUMS = HEADS * (D + 2);          // partial sums in the workspace: accumulators, maxima, sums
+  // One CTA per SM: eight warps with three stages each where they fit, else four.
+  static constexpr int fit(int warps) { return (226 * 1024 - 6144) / (warps * (STAGE + SCALES)); }
+  static constexpr int WARPS = fit(8) >= 3 ? 8 : 4, THREADS = 32 * WARPS;
+  static constexpr int NS = fit(WARPS) > 6 ? 6 : fit(WARPS);   // stages of a warp's ring
+  static constexpr int RINGS = WARPS * NS * STAGE;
+  static constexpr size_t SMEM = 1024 + static_cast<size_t>(RINGS) + WARPS * NS * SCALES;   // (1024: alignment)
+  static constexpr int QREGS = D / 16 * 2 * NH;
+  static constexpr bool AHEAD = QREGS <= 32;            // the next piece's queries are fetched under this one
+  static_assert(NS * STAGE >= 2 * HEADS * JROW * 4, "a warp's two cut pieces fit its ring");
+  static_assert(RINGS >= 2 * kMaxCtas * HEADS * 4, "the factors of a join over all CTAs fit the rings");
+  static_assert(NS >= 2 && KV % 1024 == 0, "a ring needs two stages, a swizzled block 1024-byte alignment");
 };
 
-// Tiles of sequence of length n: those that hold a token of the window.
+// 16-byte piece `c` of row `row` in a swizzled tile.
+template <class S>
+__device__ __forceinline__ uint32_t piece_at(uint32_t tile, int row, int c) {
+  if constexpr (S::CBB == 128) return tile + (c >> 3) * (S::TT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+  return tile + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+
+__device__ __forceinline__ int clamp_len(const AttnArgs& a, int n) { return n < 0 ? 0 : n > a.max_len ? a.max_len : n; }
 __device__ __forceinline__ int first_token(const AttnArgs& a, int n) { return a.window > 0 && n > a.window ? n - a.window : 0; }
+// Tiles of a sequence of length n: those that hold a token of the window.
 template <int TT>
 __device__ __forceinline__ int tile_count(const AttnArgs& a, int n) {
   return n <= 0 ? 0 : (n - 1) / TT - first_token(a, n) / TT + 1;
 }
-__device__ __forceinline__ int clamp_len(const AttnArgs& a, int n) { return n < 0 ? 0 : n > a.max_len ? a.max_len : n; }
 
-template <int D, bool I8, int ROWS>
-__global__ void __launch_bounds__(kThreads, Shape<D, I8>::CTAS) attention_kernel(AttnArgs a) {
-  using S = Shape<D, I8>;
-  constexpr int TT = S::TT, R = S::R, NT = 2 * R, HALVES = S::HALVES, NS = S::NS;
-  constexpr int KSTEPS = D / 16;
-  extern __shared__ __align__(128) unsigned char smem[];
+// Empty places in front of the nt tiles of a (sequence, head).  `whole` != 0 (little work): they fill up the CTAs' runs of
+// `whole` places, so that no CTA has tiles of two heads.  Else kToll: what beginning and ending a head costs, in tiles.
+__device__ __forceinline__ int lead_places(int nt, int whole) { return whole ? -nt & (whole - 1) : kToll; }
+
+// Position in the list: a piece is a run of tiles of one (sequence, head), inside one warp's part.
+struct Walk {
+  int x;                // place of the piece's beginning (a launch's list has fewer than 2^31)
+  int seq, hc;          // sequence; key/value head and chunk of its query heads
+  int at, nt, lead;     // place within the (sequence, head), its tiles, the places in front of them
+  int n, begin;         // the sequence's length and first token
+  __device__ __forceinline__ int first() const { return at < lead ? 0 : at - lead; }
+  __device__ __forceinline__ int places(int x1) const {
+    const int rest = nt + lead - at;
+    return x1 - x < rest ? x1 - x : rest;
+  }
+  __device__ __forceinline__ int count(int x1) const {
+    const int end = at + places(x1) - lead;
+    return end > first() ? end - first() : 0;
+  }
+};
+
+// A cut piece: what a warp has of a (sequence, head).  Two per warp, in the order of the list: one that began in front of
+// the warp's part and ends in it (its sums are parked in the workspace while the warp goes on), and the last one (its
+// sums go to the warp's ring when that has run dry).
+struct Part {
+  int seq, hc;          // hc < 0: there is none
+  int t0, t1, nt;       // tiles of it
+  int begin;            // place of the (sequence, head)'s first tile
+};
+
+template <int D, bool I8, int NH>
+__global__ void __launch_bounds__(Shape<D, I8, NH>::THREADS, 1)
+attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+  using S = Shape<D, I8, NH>;
+  constexpr int TT = S::TT, R = S::R, HALVES = S::HALVES, NS = S::NS, HEADS = S::HEADS, WIN = S::WIN;
+  constexpr int KSTEPS = D / 16, MT = D / 16, kWarps = S::WARPS, kThreads = S::THREADS;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  __shared__ __align__(8) unsigned long long s_bar[kWarps][NS];
   __shared__ int s_len[kThreads];
-  __shared__ long long s_scan[kWarps + 1];
+  __shared__ int s_scan[kWarps + 1], s_sums[2][kWarps];
   __shared__ int s_bad[kWarps][NS];
-  __shared__ int s_last;
+  __shared__ float s_m[2 * kWarps][HEADS], s_l[2 * kWarps][HEADS];
+  __shared__ Part s_part[2 * kWarps];
+  __shared__ int s_last, s_empty, s_join[2], s_cta[2][2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  const uint32_t bars = smem_u32(s_bar[warp]);
+  if (lane < NS) mbar_init(bars + 8 * lane, 1);
+  mbar_init_fence();
   pdl_launch_dependents();
   pdl_wait();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int hc_count = a.heads * a.chunks;
 
-  // ---- the list of tiles: total, then this CTA's run ----
-  long long total = 0;
-  for (int base = 0; base < a.n_seqs; base += kThreads) {
-    const int s = base + tid;
-    const int n = s < a.n_seqs ? clamp_len(a, __ldcg(a.len + s)) : 0;
-    if (s < a.n_seqs && n == 0 && s % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x)) {   // nothing to attend to
-      for (int i = 0; i < a.n_q_heads * D / 8; ++i) *reinterpret_cast<uint4*>(a.out + s * a.out_stride + i * 8) = make_uint4(0, 0, 0, 0);
-      if (a.lse)
-        for (int h = 0; h < a.n_q_heads; ++h) a.lse[static_cast<long long>(s) * a.n_q_heads + h] = -INFINITY;
-    }
-    total += static_cast<long long>(tile_count<TT>(a, n)) * hc_count;
-  }
-  for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-  if (lane == 0) s_scan[warp] = total;
-  __syncthreads();
-  total = 0;
-  for (int w = 0; w < kWarps; ++w) total += s_scan[w];
-  if (total == 0) return;
-  // a CTA per kWarps tiles at most: below that the join costs more than the split saves
-  const long long want = (total + kWarps - 1) / kWarps;
-  const int ctas = static_cast<int>(want < gridDim.x ? want : gridDim.x);
-  const int cta = blockIdx.x;
-  if (cta >= ctas) return;
-  const long long x0 = cta * total / ctas, x1 = (cta + 1) * total / ctas;
-
-  // sequence that x0 lies in
-  int seq = 0, chunk_base = 0;
-  long long at = 0;   // tiles in front of `seq`
-  for (;; chunk_base += kThreads) {
-    const int s = chunk_base + tid;
-    const int n = s < a.n_seqs ? clamp_len(a, __ldcg(a.len + s)) : 0;
-    __syncthreads();
-    s_len[tid] = n;
-    const long long mine = static_cast<long long>(tile_count<TT>(a, n)) * hc_count;
-    long long incl = mine;
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(~0u, incl, o);
-      if (lane >= o) incl += up;
-    }
-    if (lane == 31) s_scan[warp] = incl;
-    __syncthreads();
-    long long before = at, chunk = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) before += s_scan[w];
-      chunk += s_scan[w];
-    }
-    const bool here = x0 >= before + incl - mine && x0 < before + incl;
-    __syncthreads();
-    if (here) {
-      s_last = tid;
-      s_scan[kWarps] = before + incl - mine;
-    }
-    __syncthreads();
-    if (x0 < at + chunk) {
-      seq = chunk_base + s_last;
-      at = s_scan[kWarps];
-      break;
-    }
-    at += chunk;
-    if (chunk_base + kThreads >= a.n_seqs) return;   // lengths that change under the call: no run to take
-  }
-
-  const uint32_t ring = smem_u32(smem) + warp * NS * S::STAGE;
-  long long x = x0;
-  while (x < x1) {
-    // ---- one piece: tiles [tile0, tile0 + count) of (seq, hc) ----
-    const int n = s_len[seq - chunk_base];
-    const int begin = first_token(a, n);
+  // ---- the list of tiles: total, this CTA's run, this warp's part of it ----
+  auto zeros = [&](int s) {   // a sequence without tokens
+#pragma unroll 1
+    for (int i = tid; i < a.n_q_heads * D / 8; i += kThreads) *reinterpret_cast<uint4*>(a.out + s * a.out_stride + i * 8) = make_uint4(0, 0, 0, 0);
+    if (a.lse)
+#pragma unroll 1
+      for (int h = tid; h < a.n_q_heads; h += kThreads) a.lse[static_cast<long long>(s) * a.n_q_heads + h] = -INFINITY;
+  };
+  const int cta = blockIdx.x, grid = gridDim.x;
+  int whole_run = 0, run = 0, x0 = 0, x1 = 0, wx0 = 0, wx1 = 0;
+  // A run of kWarps tiles of one head per CTA while there are CTAs enough, else equal runs over the ends of heads.
+  // tiles, used, filled: of all sequences, for one head: tiles, sequences that have some, tiles filled up to kWarps.
+  auto partition = [&](int tiles, int used, int filled) {
+    whole_run = static_cast<long long>(filled) * hc_count <= kWarps * grid ? kWarps : 0;
+    const int total = (whole_run ? filled : tiles + used * kToll) * hc_count;
+    run = whole_run ? kWarps : (total + grid - 1) / grid;   // places per CTA
+    if (static_cast<long long>(cta) * run >= total) return false;
+    x0 = cta * run;
+    x1 = total - x0 < run ? total : x0 + run;
+    const int each = (x1 - x0) / kWarps, more = (x1 - x0) % kWarps;   // (the first `more` warps have one place more)
+    wx0 = x0 + warp * each + (warp < more ? warp : more);
+    wx1 = wx0 + each + (warp < more);
+    return true;
+  };
+  Walk cur;
+  int chunk_base = 0;   // s_len holds the lengths of the kThreads sequences from here on
+  auto open_at = [&](int seq, int n, int place, int seq_place) {   // cur: `place` in the sequence that begins at seq_place
+    cur.seq = seq;
+    cur.x = place;
+    cur.n = n;
+    cur.begin = first_token(a, n);
+    cur.nt = tile_count<TT>(a, n);
+    cur.lead = lead_places(cur.nt, whole_run);
+    cur.hc = (place - seq_place) / (cur.nt + cur.lead);
+    cur.at = place - seq_place - cur.hc * (cur.nt + cur.lead);
+  };
+  if (a.n_seqs <= 32) {   // every warp by itself: a lane per sequence, no barrier
+    const int n = lane < a.n_seqs ? clamp_len(a, __ldcg(a.len + lane)) : 0;
+    s_len[lane] = n;   // (every warp writes the same)
+    __syncwarp();
+#pragma unroll 1
+    for (unsigned empty = __ballot_sync(~0u, lane < a.n_seqs && n == 0 && lane % grid == cta); empty; empty &= empty - 1) zeros(__ffs(empty) - 1);
     const int nt = tile_count<TT>(a, n);
-    const long long idx = x - at;
-    const int hc = static_cast<int>(idx / nt), tile0 = static_cast<int>(idx % nt);
-    const int count = static_cast<int>(x1 - x < nt - tile0 ? x1 - x : nt - tile0);
-    const int head = hc / a.chunks, q0 = (hc % a.chunks) * kChunkRows;
-    const int rows = a.group - q0 < kChunkRows ? a.group - q0 : kChunkRows;
-    const int qh = head * a.group + q0;
-    const int base_tok = (begin / TT + tile0) * TT;
-    const int mine = count > warp ? (count - warp + kWarps - 1) / kWarps : 0;   // this warp's tiles: warp, warp + kWarps, ...
-    const int* table = a.table + static_cast<long long>(seq) * a.table_stride;
-
-    // pages of the next 32 runs of 8 tokens, one per lane
-    int pages = 0, pages_from = 0;
-    auto load_pages = [&](int from) {
-      const int i = from + lane / HALVES;
-      const int tok = base_tok + (warp + i * kWarps) * TT + (lane % HALVES) * 8;
-      pages = i < mine && tok < n ? __ldcg(table + (tok >> a.page_shift)) : -1;
-      pages_from = from;
-    };
-    auto issue = [&](int i) {
-      if (i < mine) {
-        if (i - pages_from >= 32 / HALVES) load_pages(i);
-        const int slot = i % NS;
-        const uint32_t stage = ring + slot * S::STAGE;
-        const int tok0 = base_tok + (warp + i * kWarps) * TT;
-        const int from = (i - pages_from) * HALVES;
-        const unsigned bad = __ballot_sync(~0u, static_cast<unsigned>(pages) >= static_cast<unsigned>(a.n_pages));
-        if (lane == 0) s_bad[warp][slot] = (bad >> from) & ((1u << HALVES) - 1);
-        const int mask = (1 << a.page_shift) - 1;
+    const int fill = (nt + kWarps - 1) / kWarps * kWarps;
+    const int tiles = __reduce_add_sync(~0u, nt), filled = __reduce_add_sync(~0u, fill), used = __popc(__ballot_sync(~0u, nt > 0));
+    if (tiles == 0 || !partition(tiles, used, filled)) return;
+    const int places = nt ? (nt + lead_places(nt, whole_run)) * hc_count : 0;
+    int end = places;
 #pragma unroll
-        for (int c0 = 0; c0 < TT * S::CH; c0 += 32) {
-          const int c = c0 + lane, row = c / S::CH, col = c % S::CH, tok = tok0 + row;
-          const int page = __shfl_sync(~0u, pages, from + (row >> 3));
-          if (TT * S::CH % 32 == 0 || c < TT * S::CH) {
-            const bool on = tok >= begin && tok < n && static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages);
-            const long long off = on ? (((static_cast<long long>(page) * a.heads + head) << a.page_shift) + (tok & mask)) * S::ROW + col * 16 : 0;
-            cp_async16(stage + row * S::PITCH + col * 16, a.k + off, on);
-            cp_async16(stage + S::KV + row * S::PITCH + col * 16, a.v + off, on);
-          }
-        }
-        if (I8) {   // scales, four tokens to a piece
-          const int j = lane % (TT / 4), tok = tok0 + 4 * j;
-          const int page = __shfl_sync(~0u, pages, from + (j >> 1));
-          const bool on = static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages);
-          const long long off = on ? ((static_cast<long long>(page) * a.heads + head) << a.page_shift) + (tok & mask) : 0;
-          if (lane < 2 * (TT / 4)) cp_async16(stage + 2 * S::KV + lane * 16, (lane < TT / 4 ? a.ks : a.vs) + off, on);
-        }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(~0u, end, o);
+      if (lane >= o) end += up;
+    }
+    const int seq = __ffs(__ballot_sync(~0u, wx0 < end)) - 1;   // (wx0 < x1 unless the part is empty: then -1 or any)
+    const int n_seq = __shfl_sync(~0u, n, seq & 31), begin = __shfl_sync(~0u, end - places, seq & 31);
+    if (wx0 < wx1 && seq >= 0) open_at(seq, n_seq, wx0, begin);
+    else wx1 = wx0;
+  } else {
+    if (tid == 0) s_empty = 0;
+    __syncthreads();
+    int tiles = 0, used = 0, filled = 0;
+#pragma unroll 1
+    for (int base = 0; base < a.n_seqs; base += kThreads) {
+      const int s = base + tid;
+      const int n = s < a.n_seqs ? clamp_len(a, __ldcg(a.len + s)) : 0;
+      if (base == 0) s_len[tid] = n;
+      if (s < a.n_seqs && n == 0 && s % grid == cta) s_empty = 1;
+      const int nt = tile_count<TT>(a, n);
+      tiles += nt;
+      used += nt > 0;
+      filled += (nt + kWarps - 1) / kWarps * kWarps;
+    }
+    tiles = __reduce_add_sync(~0u, tiles);
+    used = __reduce_add_sync(~0u, used);
+    filled = __reduce_add_sync(~0u, filled);
+    if (lane == 0) {
+      s_scan[warp] = tiles;
+      s_sums[0][warp] = used;
+      s_sums[1][warp] = filled;
+    }
+    __syncthreads();
+    if (s_empty) {
+#pragma unroll 1
+      for (int s = cta; s < a.n_seqs; s += grid)
+        if (__ldcg(a.len + s) <= 0) zeros(s);
+    }
+    tiles = used = filled = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      tiles += s_scan[w];
+      used += s_sums[0][w];
+      filled += s_sums[1][w];
+    }
+    if (tiles == 0 || !partition(tiles, used, filled)) return;
+    // sequence that x0 lies in
+#pragma unroll 1
+    for (int at = 0;; chunk_base += kThreads) {
+      if (chunk_base) {
+        __syncthreads();
+        s_len[tid] = chunk_base + tid < a.n_seqs ? clamp_len(a, __ldcg(a.len + chunk_base + tid)) : 0;
       }
-      cp_async_commit();
-    };
+      const int nt = tile_count<TT>(a, s_len[tid]);
+      const int places = nt ? (nt + lead_places(nt, whole_run)) * hc_count : 0;
+      int end = places;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(~0u, end, o);
+        if (lane >= o) end += up;
+      }
+      __syncthreads();
+      if (lane == 31) s_scan[warp] = end;
+      __syncthreads();
+      int chunk = 0;
+      end += at;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) end += s_scan[w];
+        chunk += s_scan[w];
+      }
+      if (x0 >= end - places && x0 < end) {
+        s_last = tid;
+        s_scan[kWarps] = end - places;
+      }
+      __syncthreads();
+      if (x0 < at + chunk) {
+        open_at(chunk_base + s_last, s_len[s_last], x0, s_scan[kWarps]);
+        break;
+      }
+      at += chunk;
+      if (chunk_base + kThreads >= a.n_seqs) return;   // lengths that change under the call: no run to take
+    }
+  }
+  auto next_sequence = [&](Walk& w) {
+#pragma unroll 1
+    do {
+      if (++w.seq >= a.n_seqs) return false;   // (as above)
+      const int i = w.seq - chunk_base;
+      w.n = i < kThreads ? s_len[i] : clamp_len(a, __ldcg(a.len + w.seq));
+    } while (w.n == 0);
+    w.begin = first_token(a, w.n);
+    w.nt = tile_count<TT>(a, w.n);
+    w.lead = lead_places(w.nt, whole_run);
+    w.hc = w.at = 0;
+    return true;
+  };
+  // the next piece with tiles behind w's; w.x == wx1: there is none
+  auto advance = [&](Walk& w) {
+#pragma unroll 1
+    do {
+      w.x += w.places(wx1);
+      w.at = 0;
+      if (w.x >= wx1 || (++w.hc == hc_count && !next_sequence(w))) {
+        w.x = wx1;
+        return;
+      }
+    } while (w.count(wx1) == 0);
+  };
+  if (wx0 < wx1) {
+#pragma unroll 1
+    while (cur.x != wx0) {   // to the sequence that the part begins in
+      const int each = cur.nt + cur.lead;
+      const int end = cur.x - cur.at + (hc_count - cur.hc) * each;
+      if (wx0 < end) {
+        const int off = wx0 - (cur.x - cur.at), more = off / each;
+        cur.hc += more;
+        cur.at = off - more * each;
+        cur.x = wx0;
+        break;
+      }
+      cur.x = end;
+      if (!next_sequence(cur)) {
+        cur.x = wx1;
+        break;
+      }
+    }
+    if (cur.x < wx1 && cur.count(wx1) == 0) advance(cur);
+  } else {
+    cur.x = wx1;
+  }
 
-    load_pages(0);
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i) issue(i);
+  // ---- this warp's copies ----
+  // A window is up to WIN of them in one piece, their pages a run of 8 tokens to a lane; the next window's pages are on their
+  // way while this one's tiles are requested.
+  struct Window {
+    int pages, head, n, begin, tok, left;
+  };
+  Walk ahead = cur;
+  int ahead_j = 0;   // next tile of `ahead`'s piece
+  auto next_window = [&](Window& w) {
+    w.left = 0;
+    if (ahead.x >= wx1) return;
+    const int count = ahead.count(wx1);   // (not 0)
+    w.left = count - ahead_j < WIN ? count - ahead_j : WIN;
+    w.head = ahead.hc / a.chunks;
+    w.n = ahead.n;
+    w.begin = ahead.begin;
+    w.tok = (ahead.begin / TT + ahead.first() + ahead_j) * TT;
+    const int tok = w.tok + lane * 8;
+    w.pages = lane < w.left * HALVES && tok < w.n
+                  ? __ldcg(a.table + static_cast<long long>(ahead.seq) * a.table_stride + (tok >> a.page_shift)) : -1;
+    ahead_j += w.left;
+    if (ahead_j == count) {
+      advance(ahead);
+      ahead_j = 0;
+    }
+  };
+  Window win, win_next;
+  win.left = 0;
+  next_window(win_next);
+  int from = 0;   // lane that holds the first page of the next tile
+  const uint32_t ring = smem_u32(smem) + warp * NS * S::STAGE;
+  const uint32_t scale_ring = smem_u32(smem) + S::RINGS + warp * NS * S::SCALES;
+  // What this lane requests of a tile: a run of 2^run_shift tokens (a page's or the tile's) of one column block of the keys
+  // (kind 0) or values (1), or their scales (2, 3).
+  const int runs = TT >> a.run_shift;
+  const int my_row = (lane & (runs - 1)) << a.run_shift, which = lane / runs;
+  const int my_kind = which < 2 * S::NCB ? which / S::NCB : I8 && which < 2 * S::NCB + 2 ? which - 2 * S::NCB + 2 : 4;
+  const int my_block = which % S::NCB;
+  const uint32_t my_dst = my_kind < 2 ? my_kind * S::KV + my_block * (TT * S::CBB) + my_row * S::CBB : ((my_kind - 2) * TT + my_row) * 4;
+  int put = 0, get = 0;
+  uint32_t phase = 0;
+  int tries = kWaitTries;
+  auto issue = [&]() {
+    if (win.left == 0) {
+      win = win_next;
+      from = 0;
+      if (win.left) next_window(win_next);
+    }
+    if (win.left) {
+      const uint32_t bar = bars + 8 * put;
+      const unsigned bad = __ballot_sync(~0u, static_cast<unsigned>(win.pages) >= static_cast<unsigned>(a.n_pages));
+      const int page = __shfl_sync(~0u, win.pages, from + (my_row >> 3));
+      const bool on = my_kind < 4 && static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages);
+      const unsigned tiles = __ballot_sync(~0u, on && my_kind < 2), scales = I8 ? __ballot_sync(~0u, on && my_kind >= 2) : 0;
+      if (lane == 0) {
+        s_bad[warp][put] = (bad >> from) & ((1u << HALVES) - 1);
+        mbar_arrive_expect_tx(bar, (__popc(tiles) * S::CBB + __popc(scales) * 4) << a.run_shift);
+      }
+      __syncwarp();
+      if (on) {
+        const long long row = ((static_cast<long long>(page) * a.heads + win.head) << a.page_shift) + ((win.tok + my_row) & ((1 << a.page_shift) - 1));
+        if (my_kind < 2) tma_box_2d(ring + put * S::STAGE + my_dst, my_kind ? &v_map : &k_map, my_block * (S::CBB / (I8 ? 1 : 2)), static_cast<int>(row), bar);
+        else bulk_g2s(scale_ring + put * S::SCALES + my_dst, (my_kind == 2 ? a.ks : a.vs) + row, 4 << a.run_shift, bar);
+      }
+      win.tok += TT;
+      --win.left;
+      from += HALVES;
+      put = put + 1 == NS ? 0 : put + 1;
+    }
+  };
 
-    // queries: rows g and g + 8 of the A operand.  8-bit keys come four dimensions to a register, so the reduction slots of
-    // a step are filled in that order: slots 2t, 2t+1, 2t+8, 2t+9 hold dimensions 4t .. 4t+3.
-    uint32_t qa[KSTEPS][ROWS == 16 ? 4 : 2];
-    {
-      const __half* qrow = a.q + seq * a.q_stride + static_cast<long long>(qh) * D;
+  // Queries as the B operand: lane (g, t4) holds head g, dimensions 2 t4, +1, +8, +9 of a step; 8-bit keys come four
+  // dimensions to a register, so there a step's slots hold dimensions 4 t4 .. 4 t4 + 3 in order.
+  auto load_queries = [&](const Walk& w, uint32_t (&q)[NH][KSTEPS][2]) {
+    const int head = w.hc / a.chunks, q0 = (w.hc - head * a.chunks) * HEADS;
+    const __half* base = a.q + w.seq * a.q_stride + static_cast<long long>(head * a.group + q0) * D;
 #pragma unroll
-      for (int r = 0; r < ROWS / 8; ++r) {
-        const bool on = g + 8 * r < rows;
-        const __half* p = qrow + (g + 8 * r) * D;
+    for (int nh = 0; nh < NH; ++nh) {
+      const bool on = q0 + nh * 8 + g < a.group;
+      const __half* p = base + (nh * 8 + g) * D;
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-          uint32_t lo = 0, hi = 0;
-          if (on) {
-            if (I8) {
-              const uint2 w = __ldcg(reinterpret_cast<const uint2*>(p + ks * 16 + 4 * t4));
-              lo = w.x;
-              hi = w.y;
-            } else {
-              lo = __ldcg(reinterpret_cast<const unsigned int*>(p + ks * 16 + 2 * t4));
-              hi = __ldcg(reinterpret_cast<const unsigned int*>(p + ks * 16 + 8 + 2 * t4));
-            }
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        q[nh][ks][0] = q[nh][ks][1] = 0;
+        if (on) {
+          if (I8) {
+            const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p + ks * 16 + 4 * t4));
+            q[nh][ks][0] = v.x;
+            q[nh][ks][1] = v.y;
+          } else {
+            q[nh][ks][0] = __ldcg(reinterpret_cast<const unsigned int*>(p + ks * 16 + 2 * t4));
+            q[nh][ks][1] = __ldcg(reinterpret_cast<const unsigned int*>(p + ks * 16 + 8 + 2 * t4));
           }
-          qa[ks][r] = lo;
-          qa[ks][ROWS / 8 + r] = hi;
         }
       }
     }
+  };
 
-    float o[D / 8][4];
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+#pragma unroll 1
+  for (int i = 0; i < NS - 1; ++i) issue();
+  uint32_t q[NH][KSTEPS][2];
+  if (cur.x < wx1) load_queries(cur, q);
 
-    for (int i = 0; i < mine; ++i) {
-      cp_async_wait<NS - 2>();
-      __syncwarp();   // the tile is there, and every lane is done with the tile before it: its stage is free
-      issue(i + NS - 1);
-      const int slot = i % NS;
-      const uint32_t stage = ring + slot * S::STAGE;
-      const int tok0 = base_tok + (warp + i * kWarps) * TT;
-      const int bad = s_bad[warp][slot];
+  if (lane < 2) s_part[2 * warp + lane].hc = -1;
+#pragma unroll 1
+  while (cur.x < wx1) {
+    // ---- one piece ----
+    const int count = cur.count(wx1), tile0 = cur.first();
+    const int head = cur.hc / a.chunks, q0 = (cur.hc - head * a.chunks) * HEADS;
+    const int rows = a.group - q0 < HEADS ? a.group - q0 : HEADS;
+    Walk next = cur;
+    advance(next);
+    uint32_t qn[S::AHEAD ? NH : 1][S::AHEAD ? KSTEPS : 1][2];
+    if constexpr (S::AHEAD) {
+      if (next.x < wx1) load_queries(next, qn);
+    }
 
-      // scores
-      float sc[NT][4];
+    float o[MT][NH][4];           // [16 dimensions][8 heads]
+    float m[NH][2], l[NH][2];     // heads 2 t4, 2 t4 + 1
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+    for (int nh = 0; nh < NH; ++nh) {
+      m[nh][0] = m[nh][1] = -INFINITY;
+      l[nh][0] = l[nh][1] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[j][e] = 0.0f;
-      if (I8) {
+      for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][nh][e] = 0.0f;
+    }
+
+#pragma unroll 1
+    for (int j = 0; j < count; ++j) {
+      __syncwarp();   // every lane is done with the tile before this one: its stage is free
+      issue();
+      if (!mbar_wait(bars + 8 * get, phase, tries)) {   // (a copy that never completes: wrong output, but the kernel ends)
+        if (tries && lane == 0) atomicAdd(a.error_flag, 1);
+        tries = 0;
+      }
+      const uint32_t stage = ring + get * S::STAGE, stage_scales = scale_ring + get * S::SCALES;
+      const int tok0 = (cur.begin / TT + tile0 + j) * TT;
+      const int bad = s_bad[warp][get];
+      if (++get == NS) {
+        get = 0;
+        phase ^= 1;
+      }
+
+      // scores: sc[r][nh] = 16 tokens x 8 heads; two sums a step apart, so that fewer products wait for one another
+      float sc[R][NH][4];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[r][nh][e] = 0.0f;
+      if constexpr (I8) {
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
-          for (int r = 0; r < R / 2; ++r) {
+          for (int rr = 0; rr < R; rr += 2) {
             uint32_t b[4];
-            ldmatrix4(b, stage + (r * 32 + lane) * S::PITCH + ks * 16);
+            ldmatrix4(b, piece_at<S>(stage, rr * 16 + lane, ks));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t u = b[e] ^ 0x80808080u;
-              mma16816(sc[4 * r + e], qa[ks][0], ROWS == 16 ? qa[ks][1] : 0u, qa[ks][ROWS / 8], ROWS == 16 ? qa[ks][ROWS / 8 + 1] : 0u,
-                       bytes_to_half2<0x4140>(u), bytes_to_half2<0x4342>(u));
+            for (int e = 0; e < 4; ++e) b[e] ^= 0x80808080u;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t a0 = bytes_to_half2<0x4140>(b[2 * r]), a1 = bytes_to_half2<0x4140>(b[2 * r + 1]);
+              const uint32_t a2 = bytes_to_half2<0x4342>(b[2 * r]), a3 = bytes_to_half2<0x4342>(b[2 * r + 1]);
+#pragma unroll
+              for (int nh = 0; nh < NH; ++nh) mma16816(sc[rr + r][nh], a0, a1, a2, a3, q[nh][ks][0], q[nh][ks][1]);
             }
           }
       } else {
+        float odd[R][NH][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd[r][nh][e] = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             uint32_t b[4];
-            ldmatrix4(b, stage + (r * 16 + (lane & 7) + ((lane >> 4) << 3)) * S::PITCH + (2 * ks + ((lane >> 3) & 1)) * 16);
-            mma16816(sc[2 * r], qa[ks][0], ROWS == 16 ? qa[ks][1] : 0u, qa[ks][ROWS / 8], ROWS == 16 ? qa[ks][ROWS / 8 + 1] : 0u, b[0], b[1]);
-            mma16816(sc[2 * r + 1], qa[ks][0], ROWS == 16 ? qa[ks][1] : 0u, qa[ks][ROWS / 8], ROWS == 16 ? qa[ks][ROWS / 8 + 1] : 0u, b[2], b[3]);
+            ldmatrix4(b, piece_at<S>(stage, r * 16 + (lane & 15), 2 * ks + (lane >> 4)));
+#pragma unroll
+            for (int nh = 0; nh < NH; ++nh) mma16816(ks & 1 ? odd[r][nh] : sc[r][nh], b[0], b[1], b[2], b[3], q[nh][ks][0], q[nh][ks][1]);
           }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[r][nh][e] += odd[r][nh][e];
       }
 
       // Scale.  8-bit values are multiplied as integers: the weight of token t carries its value scale, 2^(s + log2 scale_v),
       // and the maximum is taken of that exponent, so that the largest weight is 1 whatever the scales are.
-      float lv[NT][2];
+      float lv[R][2];   // tokens g, g + 8 of a block of 16
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        float k0 = a.scale_log2, k1 = a.scale_log2;
-        if (I8) {
-          const float2 kk = *reinterpret_cast<const float2*>(smem + (stage - smem_u32(smem)) + 2 * S::KV + (8 * j + 2 * t4) * 4);
-          const float2 vv = *reinterpret_cast<const float2*>(smem + (stage - smem_u32(smem)) + 2 * S::KV + TT * 4 + (8 * j + 2 * t4) * 4);
-          k0 *= kk.x;
-          k1 *= kk.y;
-          lv[j][0] = fmaxf(log2_fast(vv.x), -40.0f);   // (a scale of 0 goes with integers of 0)
-          lv[j][1] = fmaxf(log2_fast(vv.y), -40.0f);
-          if (vv.x != vv.x) lv[j][0] = vv.x;           // (fmaxf drops a NaN)
-          if (vv.y != vv.y) lv[j][1] = vv.y;
-        } else {
-          lv[j][0] = lv[j][1] = 0.0f;
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float f = a.scale_log2;
+          lv[r][e] = 0.0f;
+          if constexpr (I8) {
+            f *= lds_f32(stage_scales + (16 * r + 8 * e + g) * 4);
+            const float v = lds_f32(stage_scales + (TT + 16 * r + 8 * e + g) * 4);
+            lv[r][e] = v != v ? v : fmaxf(log2_fast(v), -40.0f);   // (a scale of 0 goes with integers of 0)
+          }
+#pragma unroll
+          for (int nh = 0; nh < NH; ++nh) {
+            sc[r][nh][2 * e] *= f;
+            sc[r][nh][2 * e + 1] *= f;
+          }
         }
-        sc[j][0] *= k0;
-        sc[j][1] *= k1;
-        sc[j][2] *= k0;
-        sc[j][3] *= k1;
-      }
-      if (tok0 < begin || tok0 + TT > n || bad) {   // tokens that do not take part
+      if (tok0 < cur.begin || tok0 + TT > cur.n || bad) {   // tokens that do not take part
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int tok = tok0 + 8 * j + 2 * t4 + e;
-            if (tok < begin || tok >= n || ((bad >> j) & 1)) {
-              sc[j][e] = sc[j][2 + e] = -INFINITY;
-              lv[j][e] = 0.0f;
+            const int tok = tok0 + 16 * r + 8 * e + g;
+            if (tok < cur.begin || tok >= cur.n || ((bad >> (2 * r + e)) & 1)) {
+#pragma unroll
+              for (int nh = 0; nh < NH; ++nh) sc[r][nh][2 * e] = sc[r][nh][2 * e + 1] = -INFINITY;
+              lv[r][e] = 0.0f;
+            }
+          }
+        // their values become zeros: a weight of 0 does not silence an infinity or NaN
+#pragma unroll 1
+        for (int i = lane; i < TT * S::NCB * (S::CBB / 16); i += 32) {
+          const int row = i / (S::CBB / 16) % TT, tok = tok0 + row;
+          if (tok < cur.begin || tok >= cur.n || ((bad >> (row >> 3)) & 1)) sts128(stage + S::KV + i * 16, make_uint4(0, 0, 0, 0));
+        }
+        fence_proxy_async();   // (the stage's next copy comes behind these writes)
+        __syncwarp();
+      }
+
+      // running maximum
+      float top[NH][2];
+      bool up = false;
+#pragma unroll
+      for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          top[nh][h] = -INFINITY;
+#pragma unroll
+          for (int r = 0; r < R; ++r) top[nh][h] = fmaxf(top[nh][h], fmaxf(sc[r][nh][h] + lv[r][0], sc[r][nh][2 + h] + lv[r][1]));
+          up |= top[nh][h] > m[nh][h] + kSlack;
+        }
+      if (__any_sync(~0u, up)) {
+#pragma unroll
+        for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float t = top[nh][h];
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, x));
+            t = fmaxf(t, m[nh][h]);
+            const float alpha = t == -INFINITY ? 1.0f : exp2_fast(m[nh][h] - t);
+            m[nh][h] = t;
+            l[nh][h] *= alpha;
+#pragma unroll
+            for (int j2 = 0; j2 < MT; ++j2) {
+              o[j2][nh][h] *= alpha;
+              o[j2][nh][2 + h] *= alpha;
             }
           }
       }
 
-      // running maximum, weights
-      uint32_t ph[NT][ROWS / 8], pl[NT][ROWS / 8];
-      float alpha[2] = {1.0f, 1.0f};
+      // weights: each the sum of two binary16 numbers, so that 22 significant bits reach the product
+      uint32_t ph[R][NH][2], pl[R][NH][2];
 #pragma unroll
-      for (int r = 0; r < ROWS / 8; ++r) {
-        float top = m[r];
+      for (int nh = 0; nh < NH; ++nh) {
+        const float b0 = (m[nh][0] == -INFINITY ? 0.0f : m[nh][0]) - kLift, b1 = (m[nh][1] == -INFINITY ? 0.0f : m[nh][1]) - kLift;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) top = fmaxf(top, fmaxf(sc[j][2 * r] + lv[j][0], sc[j][2 * r + 1] + lv[j][1]));
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-        const float base = (top == -INFINITY ? 0.0f : top) - kLift;
-        alpha[r] = exp2_fast(m[r] - kLift - base);
-        m[r] = top;
-        float sum = 0.0f;
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const float e0 = sc[j][2 * r] - base, e1 = sc[j][2 * r + 1] - base;
-          float p0 = exp2_fast(e0), p1 = exp2_fast(e1);
-          sum += p0 + p1;
-          if (I8) {
-            p0 = exp2_fast(e0 + lv[j][0]);
-            p1 = exp2_fast(e1 + lv[j][1]);
+          for (int e = 0; e < 2; ++e) {
+            const float e0 = sc[r][nh][2 * e] - b0, e1 = sc[r][nh][2 * e + 1] - b1;
+            float p0 = exp2_fast(e0), p1 = exp2_fast(e1);
+            l[nh][0] += p0;
+            l[nh][1] += p1;
+            if constexpr (I8) {
+              p0 = exp2_fast(e0 + lv[r][e]);
+              p1 = exp2_fast(e1 + lv[r][e]);
+            }
+            const uint32_t hi = pack_half2(p0, p1);
+            const float2 back = unpack_half2(hi);
+            ph[r][nh][e] = transpose8x8(hi);
+            pl[r][nh][e] = transpose8x8(pack_half2(p0 - back.x, p1 - back.y));
           }
-          // a weight is the sum of two binary16 numbers: 22 significant bits reach the product
-          ph[j][r] = pack_half2(p0, p1);
-          const float2 back = unpack_half2(ph[j][r]);
-          pl[j][r] = pack_half2(p0 - back.x, p1 - back.y);
-        }
-        l[r] = l[r] * alpha[r] + sum;
-      }
-      if (__any_sync(~0u, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j) {
-          o[j][0] *= alpha[0];
-          o[j][1] *= alpha[0];
-          if (ROWS == 16) {
-            o[j][2] *= alpha[1];
-            o[j][3] *= alpha[1];
-          }
-        }
       }
 
       // values
-      auto weigh = [&](float (&acc)[4], int r, uint32_t b0, uint32_t b1) {
-        mma16816(acc, ph[2 * r][0], ROWS == 16 ? ph[2 * r][ROWS / 8 - 1] : 0u, ph[2 * r + 1][0], ROWS == 16 ? ph[2 * r + 1][ROWS / 8 - 1] : 0u, b0, b1);
-        mma16816(acc, pl[2 * r][0], ROWS == 16 ? pl[2 * r][ROWS / 8 - 1] : 0u, pl[2 * r + 1][0], ROWS == 16 ? pl[2 * r + 1][ROWS / 8 - 1] : 0u, b0, b1);
-      };
-      if (I8) {
-        // a transposed matrix gives a lane two adjacent dimensions of two tokens: even and odd dimensions are tiles of their own
+      if constexpr (I8) {
+        // A transposed matrix gives a lane two adjacent dimensions of two tokens: rows g of the operand are the even
+        // dimensions of a run of 16, rows g + 8 the odd ones.
 #pragma unroll
-        for (int c = 0; c < S::CH; ++c)
+        for (int c = 0; c < MT; ++c)
 #pragma unroll
-          for (int r = 0; r < R / 2; ++r) {
+          for (int rr = 0; rr < R; rr += 2) {
             uint32_t b[4];
-            ldmatrix4_trans(b, stage + S::KV + (r * 32 + lane) * S::PITCH + c * 16);
+            ldmatrix4_trans(b, piece_at<S>(stage + S::KV, rr * 16 + lane, c));
 #pragma unroll
             for (int e = 0; e < 4; ++e) b[e] ^= 0x80808080u;
-            weigh(o[2 * c], 2 * r, bytes_to_half2<0x4240>(b[0]), bytes_to_half2<0x4240>(b[1]));
-            weigh(o[2 * c + 1], 2 * r, bytes_to_half2<0x4341>(b[0]), bytes_to_half2<0x4341>(b[1]));
-            weigh(o[2 * c], 2 * r + 1, bytes_to_half2<0x4240>(b[2]), bytes_to_half2<0x4240>(b[3]));
-            weigh(o[2 * c + 1], 2 * r + 1, bytes_to_half2<0x4341>(b[2]), bytes_to_half2<0x4341>(b[3]));
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t a0 = bytes_to_half2<0x4240>(b[2 * r]), a1 = bytes_to_half2<0x4341>(b[2 * r]);
+              const uint32_t a2 = bytes_to_half2<0x4240>(b[2 * r + 1]), a3 = bytes_to_half2<0x4341>(b[2 * r + 1]);
+#pragma unroll
+              for (int nh = 0; nh < NH; ++nh) {
+                mma16816(o[c][nh], a0, a1, a2, a3, ph[rr + r][nh][0], ph[rr + r][nh][1]);
+                mma16816(o[c][nh], a0, a1, a2, a3, pl[rr + r][nh][0], pl[rr + r][nh][1]);
+              }
+            }
           }
       } else {
 #pragma unroll
-        for (int c = 0; c < D / 8; c += 2)
+        for (int c = 0; c < MT; ++c)
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             uint32_t b[4];
-            ldmatrix4_trans(b, stage + S::KV + (r * 16 + (lane & 15)) * S::PITCH + (c + (lane >> 4)) * 16);
-            weigh(o[c], r, b[0], b[1]);
-            weigh(o[c + 1], r, b[2], b[3]);
+            ldmatrix4_trans(b, piece_at<S>(stage + S::KV, r * 16 + (lane & 7) + ((lane >> 4) << 3), 2 * c + ((lane >> 3) & 1)));
+#pragma unroll
+            for (int nh = 0; nh < NH; ++nh) {
+              mma16816(o[c][nh], b[0], b[1], b[2], b[3], ph[r][nh][0], ph[r][nh][1]);
+              mma16816(o[c][nh], b[0], b[1], b[2], b[3], pl[r][nh][0], pl[r][nh][1]);
+            }
           }
       }
     }
-    cp_async_wait<0>();
 
-    // ---- the warps' sums, joined in shared memory ----
 #pragma unroll
-    for (int r = 0; r < ROWS / 8; ++r) {
-      l[r] += __shfl_xor_sync(~0u, l[r], 1);
-      l[r] += __shfl_xor_sync(~0u, l[r], 2);
+    for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[nh][h] += __shfl_xor_sync(~0u, l[nh][h], x);
+    if (count == cur.nt) {
+      // ---- all of the head: out = o / l, eight heads by sixteen dimensions turned round at a time ----
+      __half* out = a.out + cur.seq * a.out_stride + static_cast<long long>(head * a.group + q0) * D;
+      const long long out_row = static_cast<long long>(cur.seq) * a.n_q_heads + head * a.group + q0;
+#pragma unroll
+      for (int nh = 0; nh < NH; ++nh) {
+        float inv[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          inv[h] = inverse(l[nh][h]);
+          const int row = nh * 8 + 2 * t4 + h;
+          if (a.lse && g == 0 && row < rows) a.lse[out_row + row] = log_sum(m[nh][h], l[nh][h]);
+        }
+        const int row = nh * 8 + g;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const uint32_t u = transpose8x8(pack_half2(o[j][nh][0] * inv[0], o[j][nh][1] * inv[1]));
+          const uint32_t w = transpose8x8(pack_half2(o[j][nh][2] * inv[0], o[j][nh][3] * inv[1]));
+          if (row < rows) {
+            __half* d = out + row * D + 16 * j;
+            if (I8) {   // even dimensions in u, odd ones in w
+              *reinterpret_cast<uint2*>(d + 4 * t4) = make_uint2(prmt(u, w, 0x5410), prmt(u, w, 0x7632));
+            } else {
+              *reinterpret_cast<uint32_t*>(d + 2 * t4) = u;
+              *reinterpret_cast<uint32_t*>(d + 8 + 2 * t4) = w;
+            }
+          }
+        }
+      }
+    } else {
+      // ---- a cut piece: parked, or left in the ring if it is this warp's last ----
+      const int slot = 2 * warp + (next.x < wx1 ? 0 : 1);
+      float* sums = slot & 1 ? reinterpret_cast<float*>(smem + warp * NS * S::STAGE) : a.partial + static_cast<long long>(2 * kMaxCtas + cta * kMaxWarps + warp) * S::SUMS;
+      const int pitch = slot & 1 ? S::JROW : D;
+      if (slot & 1) __syncwarp();   // every lane has read the last tile
+#pragma unroll
+      for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float* row = sums + (nh * 8 + 2 * t4 + h) * pitch;
+#pragma unroll
+          for (int j = 0; j < MT; ++j) {
+            row[16 * j + (I8 ? 2 * g : g)] = o[j][nh][h];
+            row[16 * j + (I8 ? 2 * g + 1 : g + 8)] = o[j][nh][2 + h];
+          }
+          if (g == 0) {
+            s_m[slot][nh * 8 + 2 * t4 + h] = m[nh][h];
+            s_l[slot][nh * 8 + 2 * t4 + h] = l[nh][h];
+          }
+        }
+      if (lane == 0) s_part[slot] = {cur.seq, cur.hc, tile0, tile0 + count, cur.nt, cur.x - cur.at + cur.lead};
+    }
+
+    cur = next;
+    if constexpr (S::AHEAD) {
+#pragma unroll
+      for (int nh = 0; nh < NH; ++nh)
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+          q[nh][ks][0] = qn[nh][ks][0];
+          q[nh][ks][1] = qn[nh][ks][1];
+        }
+    } else {
+      if (cur.x < wx1) load_queries(cur, q);
+    }
+  }
+
+  // ---- the CTA's cut heads, in the order of the list ----
+  __syncwarp();
+  if (s_part[2 * warp].hc >= 0) {   // the parked sums come back, behind the last piece's
+    const float4* src = reinterpret_cast<const float4*>(a.partial + static_cast<long long>(2 * kMaxCtas + cta * kMaxWarps + warp) * S::SUMS);
+    unsigned char* dst = smem + warp * NS * S::STAGE + HEADS * S::JROW * 4;
+#pragma unroll 8
+    for (int i = lane; i < HEADS * (D / 4); i += 32)
+      *reinterpret_cast<float4*>(dst + (i / (D / 4) * S::JROW + i % (D / 4) * 4) * 4) = __ldcg(src + i);
+  }
+  if (tid < 2) s_join[tid] = 0;
+  __syncthreads();
+  auto finish = [&](int seq, int hc, int row, int col, float4 acc, float top, float sum) {
+    const int head = hc / a.chunks, h = head * a.group + (hc - head * a.chunks) * HEADS + row;
+    const float inv = inverse(sum);
+    *reinterpret_cast<uint2*>(a.out + seq * a.out_stride + static_cast<long long>(h) * D + col) =
+        make_uint2(pack_half2(acc.x * inv, acc.y * inv), pack_half2(acc.z * inv, acc.w * inv));
+    if (col == 0 && a.lse) a.lse[static_cast<long long>(seq) * a.n_q_heads + h] = log_sum(top, sum);
+  };
+  auto rows_of = [&](int hc) {
+    const int rest = a.group - hc % a.chunks * HEADS;
+    return rest < HEADS ? rest : HEADS;
+  };
+  // lane p looks at part p: which there are, and where another head begins
+  Part mine = s_part[lane < 2 * kWarps ? lane : 0];
+  if (lane >= 2 * kWarps) mine.hc = -1;
+  const unsigned there = __ballot_sync(~0u, mine.hc >= 0);
+  const unsigned below = there & ((1u << lane) - 1);
+  const int prev = below ? 31 - __clz(below) : lane;
+  const int prev_seq = __shfl_sync(~0u, mine.seq, prev), prev_hc = __shfl_sync(~0u, mine.hc, prev);   // (by all lanes, no && between)
+  const bool same = below != 0 && prev_seq == mine.seq && prev_hc == mine.hc;
+  const unsigned heads = __ballot_sync(~0u, mine.hc >= 0 && !same);
+  if (heads == 0) return;
+  // heads that go on in other CTAs, in front of this one's run and behind it: their first part
+  const int p_first = __ffs(heads) - 1, p_last = 31 - __clz(heads);
+  const int first_t0 = __shfl_sync(~0u, mine.t0, p_first), last_t0 = __shfl_sync(~0u, mine.t0, p_last);
+  const int last_t1 = __shfl_sync(~0u, mine.t1, 31 - __clz(there)), last_nt = __shfl_sync(~0u, mine.nt, p_last);
+  const int open0 = first_t0 ? p_first : -1, open1 = last_t0 == 0 && last_t1 < last_nt ? p_last : -1;
+  constexpr int BLOCKS = HEADS * (D / 4) / 32;   // a warp's share of a head's sums at a time
+  const int units = __popc(heads) * BLOCKS;
+#pragma unroll 1
+  for (int unit = warp; unit < units; unit += kWarps) {
+    unsigned from_here = heads;
+    for (int k = unit / BLOCKS; k; --k) from_here &= from_here - 1;
+    const int p0 = __ffs(from_here) - 1;
+    const unsigned rest = from_here & (from_here - 1);
+    const unsigned parts = there & ~((1u << p0) - 1) & (rest ? (rest & -rest) - 1 : ~0u);
+    const int seq = __shfl_sync(~0u, mine.seq, p0), hc = __shfl_sync(~0u, mine.hc, p0), nt = __shfl_sync(~0u, mine.nt, p0);
+    const int t0 = __shfl_sync(~0u, mine.t0, p0), t1 = __shfl_sync(~0u, mine.t1, 31 - __clz(parts));
+    const int i = unit % BLOCKS * 32 + lane, row = i / (D / 4), col = (i % (D / 4)) * 4;
+    if (row >= rows_of(hc)) continue;
+    // the parts are the last pieces of some warps, and at most one parked one
+    float top = -INFINITY;
+    for (unsigned m = parts; m; m &= m - 1) top = fmaxf(top, s_m[__ffs(m) - 1][row]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float4 acc = make_float4(0, 0, 0, 0);
+    float sum = 0.0f;
+    for (unsigned m = parts; m; m &= m - 1) {
+      const int p = __ffs(m) - 1;
+      const float f = exp2_fast(s_m[p][row] - base);
+      const float4 v = *reinterpret_cast<const float4*>(smem + (p >> 1) * NS * S::STAGE + ((p & 1 ? row : HEADS + row) * S::JROW + col) * 4);
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
+      sum += f * s_l[p][row];
+    }
+    if (t0 == 0 && t1 == nt) {
+      finish(seq, hc, row, col, acc, top, sum);
+    } else {
+      float* slot = a.partial + static_cast<long long>(2 * cta + (t0 == 0)) * S::SUMS;
+      __stcg(reinterpret_cast<float4*>(slot + row * D + col), acc);
+      if (col == 0) {
+        __stcg(slot + HEADS * D + row, top);
+        __stcg(slot + HEADS * D + HEADS + row, sum);
+      }
+    }
+  }
+  if (open0 < 0 && open1 < 0) return;   // (the same for every thread)
+
+  // ---- heads that are cut between CTAs c0 .. c1: the last to arrive joins them ----
+  __syncthreads();
+  if (tid < 2 && (tid ? open1 : open0) >= 0) {
+    const Part& p = s_part[tid ? open1 : open0];
+    const int c0 = p.begin / run, c1 = (p.begin + p.nt - 1) / run;
+    if (arrive(a.counters + c0) == c1 - c0) {
+      s_join[tid] = 1;
+      s_cta[tid][0] = c0;
+      s_cta[tid][1] = c1;
+      a.counters[c0] = 0;   // as it was found
+    }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    if (!s_join[k]) continue;
+    const Part p = s_part[k ? open1 : open0];
+    const int c0 = s_cta[k][0], c1 = s_cta[k][1];
+    const int rows = rows_of(p.hc);
+    const int n = c1 - c0 + 1;
+    float* f_m = reinterpret_cast<float*>(smem);          // [n][rows]: maxima, sums
+    float* f_l = f_m + n * rows;
+    auto sums_of = [&](int c) { return a.partial + static_cast<long long>(2 * (c0 + c) + (c == 0)) * S::SUMS; };
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < n * rows; i += kThreads) {
+      const float* src = sums_of(i / rows) + HEADS * D + i % rows;
+      f_m[i] = __ldcg(src);
+      f_l[i] = __ldcg(src + HEADS);
     }
     __syncthreads();
-    float* join = reinterpret_cast<float*>(smem);                        // [warp][row][D]
-    float* jm = join + kWarps * kChunkRows * D;                          // [warp][row]: maximum, then sum
-    float* jl = jm + kWarps * kChunkRows;
-#pragma unroll
-    for (int r = 0; r < ROWS / 8; ++r) {
-      float* row = join + (warp * kChunkRows + g + 8 * r) * D;
-      if (I8) {
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-          *reinterpret_cast<float4*>(row + 16 * c + 4 * t4) = make_float4(o[2 * c][2 * r], o[2 * c + 1][2 * r], o[2 * c][2 * r + 1], o[2 * c + 1][2 * r + 1]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(row + 8 * j + 2 * t4) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
-      }
-      if (t4 == 0) {
-        jm[warp * kChunkRows + g + 8 * r] = m[r];
-        jl[warp * kChunkRows + g + 8 * r] = l[r];
-      }
-    }
-    __syncthreads();
-
-    const bool whole = count == nt;
-    const long long seg0 = x - tile0, seg1 = seg0 + nt;   // the head's run in the list
-    constexpr int SLOT = kChunkRows * (D + 2);
-    float* slot = a.partial + static_cast<long long>(2 * cta + (tile0 == 0 ? 1 : 0)) * SLOT;
+#pragma unroll 1
     for (int i = tid; i < rows * (D / 4); i += kThreads) {
       const int row = i / (D / 4), col = (i % (D / 4)) * 4;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, jm[w * kChunkRows + row]);
-      const float base = top == -INFINITY ? 0.0f : top;
+      constexpr int U = 16;   // partial sums in flight
       float4 acc = make_float4(0, 0, 0, 0);
-      float sum = 0.0f;
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+      for (int u0 = 0; u0 < n; u0 += U) {
+        float4 v[U];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_fast(jm[w * kChunkRows + row] - base);
-        const float4 v = *reinterpret_cast<const float4*>(join + (w * kChunkRows + row) * D + col);
-        acc.x += f * v.x;
-        acc.y += f * v.y;
-        acc.z += f * v.z;
-        acc.w += f * v.w;
-        sum += f * jl[w * kChunkRows + row];
-      }
-      if (whole) {
-        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-        uint2 h = make_uint2(pack_half2(acc.x * inv, acc.y * inv), pack_half2(acc.z * inv, acc.w * inv));
-        *reinterpret_cast<uint2*>(a.out + seq * a.out_stride + static_cast<long long>(qh + row) * D + col) = h;
-        if (col == 0 && a.lse) a.lse[static_cast<long long>(seq) * a.n_q_heads + qh + row] = (base - kLift + log2f(sum)) * 0.693147180559945309f;
-      } else {
-        *reinterpret_cast<float4*>(slot + row * D + col) = acc;
-        if (col == 0) {
-          slot[kChunkRows * D + row] = top;
-          slot[kChunkRows * D + kChunkRows + row] = sum;
-        }
-      }
-    }
-    if (!whole) {
-      const int c0 = static_cast<int>(((seg0 + 1) * ctas - 1) / total), c1 = static_cast<int>((seg1 * ctas - 1) / total);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        const int arrived = atomicAdd(a.counters + c0, 1);
-        s_last = arrived == c1 - c0;
-        if (s_last) a.counters[c0] = 0;   // as it was found
-      }
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        for (int i = tid; i < rows * (D / 4); i += kThreads) {
-          const int row = i / (D / 4), col = (i % (D / 4)) * 4;
-          float top = -INFINITY;
-          for (int c = c0; c <= c1; ++c)
-            top = fmaxf(top, __ldcg(a.partial + static_cast<long long>(2 * c + (c == c0)) * SLOT + kChunkRows * D + row));
-          const float base = top == -INFINITY ? 0.0f : top;
-          float4 acc = make_float4(0, 0, 0, 0);
-          float sum = 0.0f;
-          for (int c = c0; c <= c1; ++c) {
-            const float* p = a.partial + static_cast<long long>(2 * c + (c == c0)) * SLOT;
-            const float f = exp2_fast(__ldcg(p + kChunkRows * D + row) - base);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p + row * D + col));
-            acc.x += f * v.x;
-            acc.y += f * v.y;
-            acc.z += f * v.z;
-            acc.w += f * v.w;
-            sum += f * __ldcg(p + kChunkRows * D + kChunkRows + row);
+        for (int u = 0; u < U; ++u)
+          if (u0 + u < n) v[u] = __ldcg(reinterpret_cast<const float4*>(sums_of(u0 + u) + row * D + col));
+        if (u0 == 0)
+#pragma unroll 1
+          for (int u = 0; u < n; ++u) top = fmaxf(top, f_m[u * rows + row]);
+        const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u0 + u < n) {
+            const float f = exp2_fast(f_m[(u0 + u) * rows + row] - base);
+            acc.x += f * v[u].x;
+            acc.y += f * v[u].y;
+            acc.z += f * v[u].z;
+            acc.w += f * v[u].w;
+            sum += f * f_l[(u0 + u) * rows + row];
           }
-          const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-          uint2 h = make_uint2(pack_half2(acc.x * inv, acc.y * inv), pack_half2(acc.z * inv, acc.w * inv));
-          *reinterpret_cast<uint2*>(a.out + seq * a.out_stride + static_cast<long long>(qh + row) * D + col) = h;
-          if (col == 0 && a.lse) a.lse[static_cast<long long>(seq) * a.n_q_heads + qh + row] = (base - kLift + log2f(sum)) * 0.693147180559945309f;
-        }
       }
-    }
-    __syncthreads();   // the join's memory is the rings' again, s_last is free
-
-    // ---- next piece ----
-    x += count;
-    if (x < x1 && x == at + static_cast<long long>(nt) * hc_count) {
-      at = x;
-      do {
-        if (++seq >= a.n_seqs) return;   // (as above)
-        if (seq - chunk_base >= kThreads) {
-          chunk_base += kThreads;
-          __syncthreads();
-          s_len[tid] = chunk_base + tid < a.n_seqs ? clamp_len(a, __ldcg(a.len + chunk_base + tid)) : 0;
-          __syncthreads();
-        }
-      } while (s_len[seq - chunk_base] == 0);
+      finish(p.seq, p.hc, row, col, acc, top, sum);
     }
   }
 }
 
-template <int D, bool I8, int ROWS>
-vq_status launch(const AttnArgs& a, int sms, long long tiles, cudaStream_t s) {
-  using S = Shape<D, I8>;
+template <int D, bool I8, int NH>
+vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, cudaStream_t s) {
+  using S = Shape<D, I8, NH>;
   static int ready[kMaxDevices] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return VQ_ERR_CUDA;
-  auto kernel = attention_kernel<D, I8, ROWS>;
+  auto kernel = attention_kernel<D, I8, NH>;
   if (!__atomic_load_n(&ready[dev], __ATOMIC_ACQUIRE)) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::SMEM)) != cudaSuccess) return VQ_ERR_CUDA;
     __atomic_store_n(&ready[dev], 1, __ATOMIC_RELEASE);
   }
-  long long ctas = static_cast<long long>(sms) * S::CTAS;
-  if (ctas > kMaxCtas) ctas = kMaxCtas;
-  const long long most = (tiles + kWarps - 1) / kWarps;   // tiles: as many as there can be
-  if (ctas > most) ctas = most;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(kThreads), S::SMEM, s, a);
+  // the pools as matrices of tokens; a box is a column block of the tokens that a page and a tile have in common
+  while ((1 << a.run_shift) < S::TT && a.run_shift < a.page_shift) ++a.run_shift;
+  CUtensorMap maps[2];
+  const uint64_t dims[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(g.n_pages) * g.heads << g.page_shift};
+  const uint64_t strides[1] = {static_cast<uint64_t>(S::ROW)};
+  const uint32_t box[2] = {static_cast<uint32_t>(S::CBB / (I8 ? 1 : 2)), 1u << a.run_shift};
+  if (dims[1] > 0x7fffffffu) return VQ_ERR_UNSUPPORTED;
+  for (int i = 0; i < 2; ++i) {
+    const vq_status st = encode_tensor_map(&maps[i], i ? pool.v : pool.k, I8 ? 1 : 2, 2, dims, strides, box, S::CBB == 128 ? 2 : 1);
+    if (st != VQ_OK) return st;
+  }
+  a.chunks = (a.group + S::HEADS - 1) / S::HEADS;
+  const int span = a.window > 0 && a.window < a.max_len ? a.window + S::TT : a.max_len;
+  const long long each = (static_cast<long long>(span) + S::TT - 1) / S::TT;   // tiles of a head, as many as there can be
+  const long long per_seq = ((each + S::WARPS - 1) / S::WARPS * S::WARPS + kToll) * a.heads * a.chunks;
+  if (per_seq > 0x3fffffff) return VQ_ERR_UNSUPPORTED;
+  // as many sequences at a time as have places below 2^30 (tens of terabytes of cache: one launch is what there is)
+  const long long seqs = 0x3fffffff / per_seq;
+  for (long long from = 0, all = a.n_seqs; from < all; from += seqs) {
+    a.n_seqs = static_cast<int>(all - from < seqs ? all - from : seqs);
+    const long long most = per_seq * a.n_seqs / S::WARPS;
+    long long ctas = sms < kMaxCtas ? sms : kMaxCtas;
+    if (ctas > most) ctas = most;
+    const vq_status st = launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(S::THREADS), S::SMEM, s, a, maps[0], maps[1]);
+    if (st != VQ_OK) return st;
+    a.len += a.n_seqs;
+    a.table += static_cast<long long>(a.n_seqs) * a.table_stride;
+    a.q += a.n_seqs * a.q_stride;
+    a.out += a.n_seqs * a.out_stride;
+    if (a.lse) a.lse += static_cast<long long>(a.n_seqs) * a.n_q_heads;
+  }
+  return VQ_OK;
 }
 
 template <int D>
-vq_status launch_dim(const AttnArgs& a, bool int8, int sms, cudaStream_t s) {
-  const int tt = int8 ? Shape<D, true>::TT : Shape<D, false>::TT;
-  const int span = a.window > 0 && a.window < a.max_len ? a.window + tt : a.max_len;
-  const long long tiles = (static_cast<long long>(span) + tt - 1) / tt * a.heads * a.chunks * a.n_seqs;
-  if (a.group <= 8) return int8 ? launch<D, true, 8>(a, sms, tiles, s) : launch<D, false, 8>(a, sms, tiles, s);
-  return int8 ? launch<D, true, 16>(a, sms, tiles, s) : launch<D, false, 16>(a, sms, tiles, s);
+vq_status launch_dim(const AttnArgs& a, const KvGeometry& g, const KvPool& pool, int sms, cudaStream_t s) {
+  if (a.group <= 8) return g.int8 ? launch<D, true, 1>(a, g, pool, sms, s) : launch<D, false, 1>(a, g, pool, sms, s);
+  return g.int8 ? launch<D, true, 2>(a, g, pool, sms, s) : launch<D, false, 2>(a, g, pool, sms, s);
 }
 
 }  // namespace
@@ -591,20 +986,21 @@ bool kv_attention_covers(const KvGeometry& g) {
   return g.dim == 64 || g.dim == 80 || g.dim == 96 || g.dim == 128 || g.dim == 192 || g.dim == 256;
 }
 
-// Counters (one per CTA, at the start), then two slots of partial sums per CTA.
+// Counters (one per CTA, at the start), two slots of partial sums per CTA, a parking slot per warp.
 size_t kv_attention_workspace_bytes(int head_dim) {
-  return kMaxCtas * sizeof(int) + static_cast<size_t>(kMaxCtas) * 2 * kChunkRows * (head_dim + 2) * sizeof(float);
+  return kMaxCtas * sizeof(int) + static_cast<size_t>(kMaxCtas) * (2 + kMaxWarps) * kMaxHeads * (head_dim + 2) * sizeof(float);
 }
 
 vq_status launch_kv_attention(const KvGeometry& g, const KvPool& pool, const KvBooks& books, int n_q_heads, const __half* q,
                               long long q_stride, __half* out, long long out_stride, float* lse, float scale, int window, void* ws,
                               cudaStream_t s) {
   int sms = 0;
-  const vq_status st = device_sms(&sms);
+  vq_status st = device_sms(&sms);
   if (st != VQ_OK) return st;
   AttnArgs a = {};
-  a.k = pool.k;
-  a.v = pool.v;
+  st = device_error_counter(&a.error_flag);
+  if (st != VQ_OK) return st;
+  a.run_shift = 3;
   a.ks = pool.ks;
   a.vs = pool.vs;
   a.table = books.table;
@@ -623,17 +1019,16 @@ vq_status launch_kv_attention(const KvGeometry& g, const KvPool& pool, const KvB
   a.page_shift = g.page_shift;
   a.heads = g.heads;
   a.group = n_q_heads / g.heads;
-  a.chunks = (a.group + kChunkRows - 1) / kChunkRows;
   a.n_q_heads = n_q_heads;
   a.window = window;
   a.scale_log2 = scale * 1.44269504088896341f;
   switch (g.dim) {
-    case 64: return launch_dim<64>(a, g.int8, sms, s);
-    case 80: return launch_dim<80>(a, g.int8, sms, s);
-    case 96: return launch_dim<96>(a, g.int8, sms, s);
-    case 128: return launch_dim<128>(a, g.int8, sms, s);
-    case 192: return launch_dim<192>(a, g.int8, sms, s);
-    case 256: return launch_dim<256>(a, g.int8, sms, s);
+    case 64: return launch_dim<64>(a, g, pool, sms, s);
+    case 80: return launch_dim<80>(a, g, pool, sms, s);
+    case 96: return launch_dim<96>(a, g, pool, sms, s);
+    case 128: return launch_dim<128>(a, g, pool, sms, s);
+    case 192: return launch_dim<192>(a, g, pool, sms, s);
+    case 256: return launch_dim<256>(a, g, pool, sms, s);
   }
   return VQ_ERR_UNSUPPORTED;
 }
