@@ -16,7 +16,7 @@ vq_status check_kv_format(const vq_kv_format* f, KvGeometry* g) {
   while (shift < 8 && (1 << shift) != f->page_tokens) ++shift;
   if ((1 << shift) != f->page_tokens) return VQ_ERR_FORMAT;
   if (f->head_dim < 16 || f->head_dim > 256 || f->head_dim % 16) return VQ_ERR_FORMAT;
-  if (f->n_pages <= 0 || f->n_kv_heads <= 0 || f->n_kv_heads > 65536) return VQ_ERR_SHAPE;
+  if (f->n_pages <= 0 || f->n_pages > (1 << 30) || f->n_kv_heads <= 0 || f->n_kv_heads > 65536) return VQ_ERR_SHAPE;
   g->n_pages = f->n_pages;
   g->page_tokens = f->page_tokens;
   g->page_shift = shift;

@@ -2,8 +2,8 @@
 //
 //   (a, b) -> (a cos - b sin, b cos + a sin),   8-bit rows: scale = max|x| / 127, integer = rint(x / scale).
 //
-// Bound by memory: every row is read once and written once.  A CTA serves one token and a share of its heads, so the
-// token's cosines and sines are fetched once per thread and used for all of them.  A group of LG lanes holds a head's row:
+// Bound by memory: every row is read once and written once.  A CTA serves one token, or (few tokens) a share of one's heads,
+// so the token's cosines and sines are fetched once per thread and used for all of them.  A group of LG lanes holds a head's row:
 // a lane two 16-byte pieces, the two halves of the pairs that it turns, so that nothing crosses lanes but the 8-bit
 // row's maximum.
 #include "vq_device.cuh"
@@ -14,7 +14,7 @@ namespace {
 
 using namespace dev;
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 128;   // of a CTA at most
 
 struct AppendArgs {
   KvGeometry g;
@@ -42,8 +42,7 @@ __device__ __forceinline__ int sequence_of(const int* starts, int n_seqs, int to
   return lo;
 }
 
-__device__ __forceinline__ void load8(const __half* p, float (&x)[8]) {
-  const uint4 w = __ldcg(reinterpret_cast<const uint4*>(p));
+__device__ __forceinline__ void unpack8(uint4 w, float (&x)[8]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -67,6 +66,31 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, token = blockIdx.x;
+  // this lane's two pieces of eight dimensions
+  const int p = threadIdx.x % LG, pairs = a.g.dim / 16, turned = a.rot.cs ? a.rot.rot_dim / 16 : 0;
+  const bool act = p < pairs, turn = p < turned;
+  int d0 = 16 * p, d1 = 16 * p + 8;
+  if (turn && !a.rot.interleaved) {
+    d0 = 8 * p;
+    d1 = 8 * (p + turned);
+  }
+  const int heads = a.rot.n_q_heads + 2 * a.g.heads;
+  const int STEP = blockDim.x / LG;
+  const int rounds = (heads + STEP - 1) / STEP;   // (every lane takes part in every round's shuffles)
+  // a round's rows, requested a round ahead: the first ones before it is known where they go
+  uint4 raw[2];
+  auto request = [&](int round) {
+    const int h = round * STEP + threadIdx.x / LG;
+    raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
+    if (h >= heads || !act) return;
+    const int kv = h - a.rot.n_q_heads;
+    const __half* src = kv < 0 ? a.rot.q + token * a.rot.q_stride + static_cast<long long>(h) * a.g.dim
+                      : kv < a.g.heads ? a.k + token * a.k_stride + static_cast<long long>(kv) * a.g.dim
+                                       : a.v + token * a.v_stride + static_cast<long long>(kv - a.g.heads) * a.g.dim;
+    raw[0] = __ldcg(reinterpret_cast<const uint4*>(src + d0));
+    raw[1] = __ldcg(reinterpret_cast<const uint4*>(src + d1));
+  };
+  request(blockIdx.y);
   int seq = token, start = token, end = token + 1;
   if (a.starts) {
     seq = sequence_of(a.starts, a.books.n_seqs, token, lane);
@@ -83,14 +107,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
   const bool on_page = static_cast<unsigned>(page) < static_cast<unsigned>(a.g.n_pages);
   const long long slot = ((static_cast<long long>(page) * a.g.heads) << a.g.page_shift) + (pos & (a.g.page_tokens - 1));
 
-  // this lane's two pieces of eight dimensions, and what turns them
-  const int p = threadIdx.x % LG, pairs = a.g.dim / 16, turned = a.rot.cs ? a.rot.rot_dim / 16 : 0;
-  const bool act = p < pairs, turn = p < turned;
-  int d0 = 16 * p, d1 = 16 * p + 8;
-  if (turn && !a.rot.interleaved) {
-    d0 = 8 * p;
-    d1 = 8 * (p + turned);
-  }
+  // what turns this lane's pieces
   float cs[8], sn[8];
   if (turn) {
     const float4* row = reinterpret_cast<const float4*>(a.rot.cs + static_cast<long long>(pos) * (a.rot.rot_dim / 2) + 8 * p);
@@ -123,29 +140,22 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
     }
   };
 
-  const int heads = a.rot.n_q_heads + 2 * a.g.heads;
-  constexpr int STEP = kAppendThreads / LG;
-  const int rounds = (heads + STEP - 1) / STEP;   // (every lane takes part in every round's shuffles)
   for (int round = blockIdx.y; round < rounds; round += gridDim.y) {
     const int h = round * STEP + threadIdx.x / LG;
     const bool mine = h < heads && act;
     const int kv = h - a.rot.n_q_heads;             // < 0: a query head
     const bool value = kv >= a.g.heads;
     const int head = value ? kv - a.g.heads : kv;
-    int e0 = d0, e1 = d1;
-    float x[8] = {}, y[8] = {};
-    if (mine) {
-      const __half* src = kv < 0 ? a.rot.q + token * a.rot.q_stride + static_cast<long long>(h) * a.g.dim
-                                 : (value ? a.v + token * a.v_stride : a.k + token * a.k_stride) + static_cast<long long>(head) * a.g.dim;
-      load8(src + e0, x);
-      load8(src + e1, y);
-      if (turn && !value) rotate(x, y);
-    }
+    float x[8], y[8];
+    unpack8(raw[0], x);
+    unpack8(raw[1], y);
+    if (round + static_cast<int>(gridDim.y) < rounds) request(round + gridDim.y);
+    if (turn && !value) rotate(x, y);
     if (kv < 0) {
       if (mine) {
         __half* dst = a.rot.q_out + token * a.rot.q_out_stride + static_cast<long long>(h) * a.g.dim;
-        store8(dst + e0, x);
-        store8(dst + e1, y);
+        store8(dst + d0, x);
+        store8(dst + d1, y);
       }
     }
     const long long at = slot + (static_cast<long long>(head) << a.g.page_shift);   // row of the pool
@@ -162,39 +172,44 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
       if (mine && kv >= 0 && on_page) {
         const float scale = __fdiv_rn(__uint_as_float(top), 127.0f);
         uint32_t w[4] = {0, 0, 0, 0};
+        const float inv = __fdiv_rn(1.0f, scale);
         if (scale > 0.0f) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int u = max(-127, min(127, __float2int_rn(__fdiv_rn(x[i], scale))));
-            const int r = max(-127, min(127, __float2int_rn(__fdiv_rn(y[i], scale))));
+            const int u = max(-127, min(127, __float2int_rn(x[i] * inv)));
+            const int r = max(-127, min(127, __float2int_rn(y[i] * inv)));
             w[i / 4] |= static_cast<uint32_t>(u & 255) << (8 * (i % 4));
             w[2 + i / 4] |= static_cast<uint32_t>(r & 255) << (8 * (i % 4));
           }
         }
         uint8_t* dst = (value ? a.pool.v : a.pool.k) + at * a.g.dim;
-        *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
-        *reinterpret_cast<uint2*>(dst + e1) = make_uint2(w[2], w[3]);
+        *reinterpret_cast<uint2*>(dst + d0) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(dst + d1) = make_uint2(w[2], w[3]);
         if (p == 0) (value ? a.pool.vs : a.pool.ks)[at] = top >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : scale;
       }
     } else if (mine && kv >= 0 && on_page) {
       __half* dst = reinterpret_cast<__half*>(value ? a.pool.v : a.pool.k) + at * a.g.dim;
-      store8(dst + e0, x);
-      store8(dst + e1, y);
+      store8(dst + d0, x);
+      store8(dst + d1, y);
     }
   }
 }
 
 template <bool I8>
 vq_status launch(const AppendArgs& a, int n_tokens, int sms, cudaStream_t s) {
-  const int lg = a.g.dim <= 64 ? 4 : a.g.dim <= 128 ? 8 : 16;
-  const int rounds = (a.rot.n_q_heads + 2 * a.g.heads + kAppendThreads / lg - 1) / (kAppendThreads / lg);
-  // few tokens: a token's heads are spread over CTAs until there are two per SM
+  const int lg = a.g.dim <= 64 ? 4 : a.g.dim <= 128 ? 8 : 16, lanes = (a.rot.n_q_heads + 2 * a.g.heads) * lg;
+  // A token's rows wait for a chain of reads (its sequence, length, page), so many tokens want small CTAs, more of them on an SM
+  // (8192 tokens of 80 heads of 128 into 8-bit pages with 128 / 64 / 32 threads: 62 / 58 / 57 us, of 16 heads 26 / 18 / 16);
+  // of 1000 tokens every lane is needed (10.6 / 12.2 / 18.3), and with few a token's heads are spread over CTAs until
+  // there are two per SM.
+  const int threads = n_tokens > 24 * sms ? 32 : n_tokens > 8 * sms ? 64 : 128;
+  const int rounds = (lanes + threads - 1) / threads;
   int split = 2 * sms / n_tokens;
   split = split < 1 ? 1 : split > rounds ? rounds : split;
-  const dim3 grid(static_cast<unsigned>(n_tokens), static_cast<unsigned>(split));
-  if (lg == 4) return launch_dependent(append_kernel<I8, 4>, grid, dim3(kAppendThreads), 0, s, a);
-  if (lg == 8) return launch_dependent(append_kernel<I8, 8>, grid, dim3(kAppendThreads), 0, s, a);
-  return launch_dependent(append_kernel<I8, 16>, grid, dim3(kAppendThreads), 0, s, a);
+  const dim3 grid(static_cast<unsigned>(n_tokens), static_cast<unsigned>(split)), block(static_cast<unsigned>(threads));
+  if (lg == 4) return launch_dependent(append_kernel<I8, 4>, grid, block, 0, s, a);
+  if (lg == 8) return launch_dependent(append_kernel<I8, 8>, grid, block, 0, s, a);
+  return launch_dependent(append_kernel<I8, 16>, grid, block, 0, s, a);
 }
 
 }  // namespace
