@@ -30,7 +30,7 @@ constexpr int kToll = 2;                // places in front of a head's tiles: wh
 constexpr int kWaitTries = 1 << 18;     // mbarrier polls before a warp gives up and flags an error
 constexpr int kMaxHeads = 16;           // query heads that a CTA takes together at most
 constexpr int kMaxCtas = 256;          // CTAs of a launch, one per SM (partial sums and counters are sized for them)
-constexpr int kMaxWarps = 8;
+constexpr int kMaxWarps = 12;
 // Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, and two binary16 pieces hold a weight of
 // 2^-18 of the largest to 2^-32 of it.
 constexpr float kLift = 7.0f, kSlack = 8.0f;
@@ -61,6 +61,12 @@ __device__ __forceinline__ int arrive(int* counter) {
   int old;
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
   return old;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ float lds_f32(uint32_t addr) {
   float v;
@@ -112,7 +118,7 @@ struct Shape {
   static constexpr int CBB = ROW <= 64 ? 64 : 128;
   static constexpr int NCB = (ROW + CBB - 1) / CBB;
   // tokens per tile: a stage of a warp holds about 8 KB of keys and values
-  static constexpr int R = I8 ? (ROW <= 64 ? 4 : 2) : (ROW <= 128 ? 2 : 1);
+  static constexpr int R = I8 ? (ROW <= 64 ? 4 : ROW <= 128 ? 2 : 1) : (ROW <= 128 ? 2 : 1);
   static constexpr int TT = 16 * R;
   static constexpr int HALVES = TT / 8;                 // runs of 8 tokens: never across a page
   static constexpr int WIN = 32 / HALVES;               // tiles whose pages a warp's lanes hold
@@ -122,9 +128,10 @@ struct Shape {
   static constexpr int HEADS = 8 * NH;
   static constexpr int JROW = D + 4;                    // a row of the join's sums: heads of a lane's neighbours in different banks
   static constexpr int SUMS = HEADS * (D + 2);          // partial sums in the workspace: accumulators, maxima, sums
-  // One CTA per SM: eight warps with three stages each where they fit, else four.
+  // One CTA per SM: eight warps with three stages each where they fit, else four.  8-bit tiles take twice the instructions a byte
+  // (25 a token: bytes become binary16 for both products), so they get twelve warps with two stages.
   static constexpr int fit(int warps) { return (226 * 1024 - 6144) / (warps * (STAGE + SCALES)); }
-  static constexpr int WARPS = fit(8) >= 3 ? 8 : 4, THREADS = 32 * WARPS;
+  static constexpr int WARPS = I8 && NH == 1 && D <= 128 && fit(12) >= 2 ? 12 : fit(8) >= 3 && 3 * STAGE >= 2 * HEADS * JROW * 4 ? 8 : 4, THREADS = 32 * WARPS;
   static constexpr int NS = fit(WARPS) > 6 ? 6 : fit(WARPS);   // stages of a warp's ring
   static constexpr int RINGS = WARPS * NS * STAGE;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(RINGS) + WARPS * NS * SCALES;   // (1024: alignment)
@@ -152,7 +159,7 @@ __device__ __forceinline__ int tile_count(const AttnArgs& a, int n) {
 
 // Empty places in front of the nt tiles of a (sequence, head).  `whole` != 0 (little work): they fill up the CTAs' runs of
 // `whole` places, so that no CTA has tiles of two heads.  Else kToll: what beginning and ending a head costs, in tiles.
-__device__ __forceinline__ int lead_places(int nt, int whole) { return whole ? -nt & (whole - 1) : kToll; }
+__device__ __forceinline__ int lead_places(int nt, int whole) { return whole ? (whole - 1) - (nt + whole - 1) % whole : kToll; }
 
 // Position in the list: a piece is a run of tiles of one (sequence, head), inside one warp's part.
 struct Walk {
@@ -197,7 +204,7 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
   __shared__ int s_last, s_empty, s_join[2], s_cta[2][2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const uint32_t bars = smem_u32(s_bar[warp]);
-  if (lane < NS) mbar_init(bars + 8 * lane, 1);
+  if (lane < NS) mbar_init(bars + 8 * lane, I8 ? 33 : 1);   // (8-bit: every lane arrives with its part of the scales)
   mbar_init_fence();
   pdl_launch_dependents();
   pdl_wait();
@@ -416,12 +423,13 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
   const uint32_t ring = smem_u32(smem) + warp * NS * S::STAGE;
   const uint32_t scale_ring = smem_u32(smem) + S::RINGS + warp * NS * S::SCALES;
   // What this lane requests of a tile: a run of 2^run_shift tokens (a page's or the tile's) of one column block of the keys
-  // (kind 0) or values (1), or their scales (2, 3).
+  // (kind 0) or values (1).  Scales come by 16-byte copies of their own: requests of a few bytes are as dear to the copy engine
+  // as boxes.
   const int runs = TT >> a.run_shift;
   const int my_row = (lane & (runs - 1)) << a.run_shift, which = lane / runs;
-  const int my_kind = which < 2 * S::NCB ? which / S::NCB : I8 && which < 2 * S::NCB + 2 ? which - 2 * S::NCB + 2 : 4;
+  const int my_kind = which < 2 * S::NCB ? which / S::NCB : 2;
   const int my_block = which % S::NCB;
-  const uint32_t my_dst = my_kind < 2 ? my_kind * S::KV + my_block * (TT * S::CBB) + my_row * S::CBB : ((my_kind - 2) * TT + my_row) * 4;
+  const uint32_t my_dst = my_kind * S::KV + my_block * (TT * S::CBB) + my_row * S::CBB;
   int put = 0, get = 0;
   uint32_t phase = 0;
   int tries = kWaitTries;
@@ -435,17 +443,26 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
       const uint32_t bar = bars + 8 * put;
       const unsigned bad = __ballot_sync(~0u, static_cast<unsigned>(win.pages) >= static_cast<unsigned>(a.n_pages));
       const int page = __shfl_sync(~0u, win.pages, from + (my_row >> 3));
-      const bool on = my_kind < 4 && static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages);
-      const unsigned tiles = __ballot_sync(~0u, on && my_kind < 2), scales = I8 ? __ballot_sync(~0u, on && my_kind >= 2) : 0;
+      const bool on = my_kind < 2 && static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages);
+      const unsigned boxes = __ballot_sync(~0u, on);
       if (lane == 0) {
         s_bad[warp][put] = (bad >> from) & ((1u << HALVES) - 1);
-        mbar_arrive_expect_tx(bar, (__popc(tiles) * S::CBB + __popc(scales) * 4) << a.run_shift);
+        mbar_arrive_expect_tx(bar, (__popc(boxes) * S::CBB) << a.run_shift);
       }
       __syncwarp();
       if (on) {
         const long long row = ((static_cast<long long>(page) * a.heads + win.head) << a.page_shift) + ((win.tok + my_row) & ((1 << a.page_shift) - 1));
-        if (my_kind < 2) tma_box_2d(ring + put * S::STAGE + my_dst, my_kind ? &v_map : &k_map, my_block * (S::CBB / (I8 ? 1 : 2)), static_cast<int>(row), bar);
-        else bulk_g2s(scale_ring + put * S::SCALES + my_dst, (my_kind == 2 ? a.ks : a.vs) + row, 4 << a.run_shift, bar);
+        tma_box_2d(ring + put * S::STAGE + my_dst, my_kind ? &v_map : &k_map, my_block * (S::CBB / (I8 ? 1 : 2)), static_cast<int>(row), bar);
+      }
+      if constexpr (I8) {   // four tokens to a piece
+        constexpr int PIECES = TT / 4;
+        const int j = lane % PIECES, tok = win.tok + 4 * j;
+        const int its_page = __shfl_sync(~0u, win.pages, from + (j >> 1));
+        if (lane < 2 * PIECES && static_cast<unsigned>(its_page) < static_cast<unsigned>(a.n_pages)) {
+          const long long row = ((static_cast<long long>(its_page) * a.heads + win.head) << a.page_shift) + (tok & ((1 << a.page_shift) - 1));
+          cp_async16(scale_ring + put * S::SCALES + lane * 16, (lane < PIECES ? a.ks : a.vs) + row);
+        }
+        cp_async_arrive(bar);   // when the lane's copy, if any, has come
       }
       win.tok += TT;
       --win.left;
@@ -536,20 +553,23 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
 #pragma unroll
           for (int e = 0; e < 4; ++e) sc[r][nh][e] = 0.0f;
       if constexpr (I8) {
+        // four matrices at a time: a piece of 32 tokens, or two pieces of 16
+        constexpr int KJ = R == 1 ? 2 : 1;
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks)
+        for (int ks = 0; ks < KSTEPS; ks += KJ)
 #pragma unroll
           for (int rr = 0; rr < R; rr += 2) {
             uint32_t b[4];
-            ldmatrix4(b, piece_at<S>(stage, rr * 16 + lane, ks));
+            ldmatrix4(b, R == 1 ? piece_at<S>(stage, lane & 15, ks + (lane >> 4)) : piece_at<S>(stage, rr * 16 + lane, ks));
 #pragma unroll
             for (int e = 0; e < 4; ++e) b[e] ^= 0x80808080u;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               const uint32_t a0 = bytes_to_half2<0x4140>(b[2 * r]), a1 = bytes_to_half2<0x4140>(b[2 * r + 1]);
               const uint32_t a2 = bytes_to_half2<0x4342>(b[2 * r]), a3 = bytes_to_half2<0x4342>(b[2 * r + 1]);
+              const int k = R == 1 ? ks + r : ks;
 #pragma unroll
-              for (int nh = 0; nh < NH; ++nh) mma16816(sc[rr + r][nh], a0, a1, a2, a3, q[nh][ks][0], q[nh][ks][1]);
+              for (int nh = 0; nh < NH; ++nh) mma16816(sc[R == 1 ? 0 : rr + r][nh], a0, a1, a2, a3, q[nh][k][0], q[nh][k][1]);
             }
           }
       } else {
@@ -679,22 +699,24 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
       if constexpr (I8) {
         // A transposed matrix gives a lane two adjacent dimensions of two tokens: rows g of the operand are the even
         // dimensions of a run of 16, rows g + 8 the odd ones.
+        constexpr int CJ = R == 1 ? 2 : 1;
 #pragma unroll
-        for (int c = 0; c < MT; ++c)
+        for (int c = 0; c < MT; c += CJ)
 #pragma unroll
           for (int rr = 0; rr < R; rr += 2) {
             uint32_t b[4];
-            ldmatrix4_trans(b, piece_at<S>(stage + S::KV, rr * 16 + lane, c));
+            ldmatrix4_trans(b, R == 1 ? piece_at<S>(stage + S::KV, lane & 15, c + (lane >> 4)) : piece_at<S>(stage + S::KV, rr * 16 + lane, c));
 #pragma unroll
             for (int e = 0; e < 4; ++e) b[e] ^= 0x80808080u;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               const uint32_t a0 = bytes_to_half2<0x4240>(b[2 * r]), a1 = bytes_to_half2<0x4341>(b[2 * r]);
               const uint32_t a2 = bytes_to_half2<0x4240>(b[2 * r + 1]), a3 = bytes_to_half2<0x4341>(b[2 * r + 1]);
+              const int j = R == 1 ? c + r : c, block = R == 1 ? 0 : rr + r;
 #pragma unroll
               for (int nh = 0; nh < NH; ++nh) {
-                mma16816(o[c][nh], a0, a1, a2, a3, ph[rr + r][nh][0], ph[rr + r][nh][1]);
-                mma16816(o[c][nh], a0, a1, a2, a3, pl[rr + r][nh][0], pl[rr + r][nh][1]);
+                mma16816(o[j][nh], a0, a1, a2, a3, ph[block][nh][0], ph[block][nh][1]);
+                mma16816(o[j][nh], a0, a1, a2, a3, pl[block][nh][0], pl[block][nh][1]);
               }
             }
           }
