@@ -859,21 +859,36 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
     const int t0 = __shfl_sync(~0u, mine.t0, p0), t1 = __shfl_sync(~0u, mine.t1, 31 - __clz(parts));
     const int i = unit % BLOCKS * 32 + lane, row = i / (D / 4), col = (i % (D / 4)) * 4;
     if (row >= rows_of(hc)) continue;
-    // the parts are the last pieces of some warps, and at most one parked one
+    // the parts are the last pieces of some warps, and at most one parked one; all are fetched before any is used
+    float pm[kWarps + 1], pl[kWarps + 1];
+    float4 v[kWarps + 1];
+    const unsigned parked = parts & 0x55555555u;
     float top = -INFINITY;
-    for (unsigned m = parts; m; m &= m - 1) top = fmaxf(top, s_m[__ffs(m) - 1][row]);
+#pragma unroll
+    for (int w = 0; w <= kWarps; ++w) {
+      const bool there_is = w < kWarps ? (parts >> (2 * w + 1)) & 1 : parked != 0;
+      const int p = w < kWarps ? 2 * w + 1 : parked ? __ffs(parked) - 1 : 0;
+      pm[w] = -INFINITY;
+      pl[w] = 0.0f;
+      v[w] = make_float4(0, 0, 0, 0);
+      if (there_is) {
+        pm[w] = s_m[p][row];
+        pl[w] = s_l[p][row];
+        v[w] = *reinterpret_cast<const float4*>(smem + (p >> 1) * NS * S::STAGE + ((p & 1 ? row : HEADS + row) * S::JROW + col) * 4);
+      }
+      top = fmaxf(top, pm[w]);
+    }
     const float base = top == -INFINITY ? 0.0f : top;
     float4 acc = make_float4(0, 0, 0, 0);
     float sum = 0.0f;
-    for (unsigned m = parts; m; m &= m - 1) {
-      const int p = __ffs(m) - 1;
-      const float f = exp2_fast(s_m[p][row] - base);
-      const float4 v = *reinterpret_cast<const float4*>(smem + (p >> 1) * NS * S::STAGE + ((p & 1 ? row : HEADS + row) * S::JROW + col) * 4);
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
-      sum += f * s_l[p][row];
+#pragma unroll
+    for (int w = 0; w <= kWarps; ++w) {
+      const float f = exp2_fast(pm[w] - base);
+      acc.x += f * v[w].x;
+      acc.y += f * v[w].y;
+      acc.z += f * v[w].z;
+      acc.w += f * v[w].w;
+      sum += f * pl[w];
     }
     if (t0 == 0 && t1 == nt) {
       finish(seq, hc, row, col, acc, top, sum);
