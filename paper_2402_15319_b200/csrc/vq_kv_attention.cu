@@ -128,10 +128,11 @@ struct Shape {
   static constexpr int HEADS = 8 * NH;
   static constexpr int JROW = D + 4;                    // a row of the join's sums: heads of a lane's neighbours in different banks
   static constexpr int SUMS = HEADS * (D + 2);          // partial sums in the workspace: accumulators, maxima, sums
-  // One CTA per SM: eight warps with three stages each where they fit, else four.  8-bit tiles take twice the instructions a byte
-  // (25 a token: bytes become binary16 for both products), so they get twelve warps with two stages.
+  // One CTA per SM.  Twelve warps with two stages each where the accumulators leave 168 registers enough (against eight with
+  // three: sixteen sequences of 40000 tokens, 64/8 heads of 128, 401 -> 393 us, in an 8-bit cache, whose bytes become binary16
+  // for both products, 228 -> 224; one sequence of 512 tokens 8.3 -> 8.8), else eight, else four.
   static constexpr int fit(int warps) { return (226 * 1024 - 6144) / (warps * (STAGE + SCALES)); }
-  static constexpr int WARPS = I8 && NH == 1 && D <= 128 && fit(12) >= 2 ? 12 : fit(8) >= 3 && 3 * STAGE >= 2 * HEADS * JROW * 4 ? 8 : 4, THREADS = 32 * WARPS;
+  static constexpr int WARPS = NH == 1 && D <= 128 && fit(12) >= 2 ? 12 : fit(8) >= 3 && 3 * STAGE >= 2 * HEADS * JROW * 4 ? 8 : 4, THREADS = 32 * WARPS;
   static constexpr int NS = fit(WARPS) > 6 ? 6 : fit(WARPS);   // stages of a warp's ring
   static constexpr int RINGS = WARPS * NS * STAGE;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(RINGS) + WARPS * NS * SCALES;   // (1024: alignment)
