@@ -598,19 +598,20 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
             for (int e = 0; e < 4; ++e) sc[r][nh][e] += odd[r][nh][e];
       }
 
-      // Scale.  8-bit values are multiplied as integers: the weight of token t carries its value scale, 2^(s + log2 scale_v),
-      // and the maximum is taken of that exponent, so that the largest weight is 1 whatever the scales are.
-      float lv[R][2];   // tokens g, g + 8 of a block of 16
+      // Scale.  8-bit values are multiplied as integers: the weight of token t carries its value scale, 2^s * scale_v, and the
+      // maximum is taken of s + log2 scale_v, so that the largest such weight is 1 whatever the scales are.
+      float lv[R][2], sv[R][2];   // log2 scale_v, scale_v of tokens g, g + 8 of a block of 16
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float f = a.scale_log2;
           lv[r][e] = 0.0f;
+          sv[r][e] = 1.0f;
           if constexpr (I8) {
             f *= lds_f32(stage_scales + (16 * r + 8 * e + g) * 4);
-            const float v = lds_f32(stage_scales + (TT + 16 * r + 8 * e + g) * 4);
-            lv[r][e] = v != v ? v : fmaxf(log2_fast(v), -40.0f);   // (a scale of 0 goes with integers of 0)
+            sv[r][e] = lds_f32(stage_scales + (TT + 16 * r + 8 * e + g) * 4);
+            lv[r][e] = fmaxf(log2_fast(sv[r][e]), -40.0f);   // (a scale of 0 goes with integers of 0)
           }
 #pragma unroll
           for (int nh = 0; nh < NH; ++nh) {
@@ -627,7 +628,7 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
             if (tok < cur.begin || tok >= cur.n || ((bad >> (2 * r + e)) & 1)) {
 #pragma unroll
               for (int nh = 0; nh < NH; ++nh) sc[r][nh][2 * e] = sc[r][nh][2 * e + 1] = -INFINITY;
-              lv[r][e] = 0.0f;
+              lv[r][e] = sv[r][e] = 0.0f;
             }
           }
         // their values become zeros: a weight of 0 does not silence an infinity or NaN
@@ -686,8 +687,8 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
             l[nh][0] += p0;
             l[nh][1] += p1;
             if constexpr (I8) {
-              p0 = exp2_fast(e0 + lv[r][e]);
-              p1 = exp2_fast(e1 + lv[r][e]);
+              p0 *= sv[r][e];   // (2^55 at most in front of a scale of 2^-40)
+              p1 *= sv[r][e];
             }
             const uint32_t hi = pack_half2(p0, p1);
             const float2 back = unpack_half2(hi);
