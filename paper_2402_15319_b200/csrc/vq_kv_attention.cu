@@ -48,7 +48,7 @@ struct AttnArgs {
   int* error_flag;
   long long q_stride, out_stride;
   int n_seqs, table_stride, max_len, n_pages, page_shift, run_shift, heads, group, chunks, n_q_heads, window;
-  float scale_log2;
+  float scale_log2, inv_grid;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -136,6 +136,8 @@ struct Shape {
   static constexpr int NS = fit(WARPS) > 6 ? 6 : fit(WARPS);   // stages of a warp's ring
   static constexpr int RINGS = WARPS * NS * STAGE;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(RINGS) + WARPS * NS * SCALES;   // (1024: alignment)
+  // Costs of a split (see choose()): measured from calls of 1 to 16 sequences, 8 to 128 heads, 100 to 4096 tokens.
+  static constexpr float JOIN_COST = 22.0f * 8192 / STAGE, RUN_COST = 31.0f * 8192 / STAGE, ALONE = I8 ? 1.11f : 0.625f;
   static constexpr int QREGS = D / 16 * 2 * NH;
   static constexpr bool AHEAD = QREGS <= 32;            // the next piece's queries are fetched under this one
   static_assert(NS * STAGE >= 2 * HEADS * JROW * 4, "a warp's two cut pieces fit its ring");
@@ -158,8 +160,8 @@ __device__ __forceinline__ int tile_count(const AttnArgs& a, int n) {
   return n <= 0 ? 0 : (n - 1) / TT - first_token(a, n) / TT + 1;
 }
 
-// Empty places in front of the nt tiles of a (sequence, head).  `whole` != 0 (little work): they fill up the CTAs' runs of
-// `whole` places, so that no CTA has tiles of two heads.  Else kToll: what beginning and ending a head costs, in tiles.
+// Empty places in front of the nt tiles of a (sequence, head).  `whole` != 0: they fill up the CTAs' runs of `whole` places, so
+// that no CTA has tiles of two heads.  Else kToll: what beginning and ending a head costs, in tiles.
 __device__ __forceinline__ int lead_places(int nt, int whole) { return whole ? (whole - 1) - (nt + whole - 1) % whole : kToll; }
 
 // Position in the list: a piece is a run of tiles of one (sequence, head), inside one warp's part.
@@ -221,19 +223,40 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
   };
   const int cta = blockIdx.x, grid = gridDim.x;
   int whole_run = 0, run = 0, x0 = 0, x1 = 0, wx0 = 0, wx1 = 0;
-  // A run of kWarps tiles of one head per CTA while there are CTAs enough, else equal runs over the ends of heads.
-  // tiles, used, filled: of all sequences, for one head: tiles, sequences that have some, tiles filled up to kWarps.
-  auto partition = [&](int tiles, int used, int filled) {
-    whole_run = static_cast<long long>(filled) * hc_count <= kWarps * grid ? kWarps : 0;
-    const int total = (whole_run ? filled : tiles + used * kToll) * hc_count;
-    run = whole_run ? kWarps : (total + grid - 1) / grid;   // places per CTA
+  // Which split?  In tiles of a CTA at its fair share of the memory's rate (0.19 us for one of 8 KB):
+  //   a CTA per head               the longest head at the rate that one SM reaches alone, or the mean and a little if that is more
+  //   an equal number of CTAs each  the longest head's part, and the join of CTAs
+  //   equal runs over heads' ends   the mean, and the join, and the sums that warps park
+  // (16 sequences of 1000 tokens, 32/8 heads of 128, by equal runs 21.1 us, by heads 16.7; of 4096 tokens 51.2 and 46.7; of
+  // 32768 tokens 328 and 338.)  tiles, used, most: of all sequences, for one head: tiles, sequences that have some, tiles of the
+  // longest.
+  auto choose = [&](int tiles, int used, int most) {
+    const int heads = used * hc_count;
+    whole_run = 0;
+    if (heads > grid) return;
+    const float mean = tiles * hc_count * a.inv_grid, run_cost = mean + S::RUN_COST;
+    const float whole_cost = fmaxf(most * S::ALONE, 1.04f * mean);
+    if (whole_cost <= run_cost) whole_run = most;
+    if (whole_cost <= kWarps + S::JOIN_COST && whole_run) return;
+    int each = static_cast<int>(__fdividef(static_cast<float>(grid), static_cast<float>(heads)));   // (heads * each <= grid)
+    if (heads * each > grid) --each;
+    const int per = static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1;
+    const int part = per > kWarps ? per : kWarps;
+    const float part_cost = part + S::JOIN_COST;
+    if (part_cost < whole_cost && part_cost <= run_cost && each * part >= most) whole_run = part;   // (so a head has `each` CTAs at most)
+  };
+  // places: of the list
+  auto partition = [&](int total) {
+    run = whole_run ? whole_run : (total + grid - 1) / grid;   // places per CTA
     if (static_cast<long long>(cta) * run >= total) return false;
     x0 = cta * run;
     x1 = total - x0 < run ? total : x0 + run;
-    const int each = (x1 - x0) / kWarps, more = (x1 - x0) % kWarps;   // (the first `more` warps have one place more)
-    wx0 = x0 + warp * each + (warp < more ? warp : more);
-    wx1 = wx0 + each + (warp < more);
     return true;
+  };
+  auto share_out = [&](int from) {   // the run's places from `from` on, to the warps
+    const int each = (x1 - from) / kWarps, more = (x1 - from) % kWarps;   // (the first `more` warps have one place more)
+    wx0 = from + warp * each + (warp < more ? warp : more);
+    wx1 = wx0 + each + (warp < more);
   };
   Walk cur;
   int chunk_base = 0;   // s_len holds the lengths of the kThreads sequences from here on
@@ -254,24 +277,38 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
 #pragma unroll 1
     for (unsigned empty = __ballot_sync(~0u, lane < a.n_seqs && n == 0 && lane % grid == cta); empty; empty &= empty - 1) zeros(__ffs(empty) - 1);
     const int nt = tile_count<TT>(a, n);
-    const int fill = (nt + kWarps - 1) / kWarps * kWarps;
-    const int tiles = __reduce_add_sync(~0u, nt), filled = __reduce_add_sync(~0u, fill), used = __popc(__ballot_sync(~0u, nt > 0));
-    if (tiles == 0 || !partition(tiles, used, filled)) return;
+    const int tiles = __reduce_add_sync(~0u, nt), most = __reduce_max_sync(~0u, nt), used = __popc(__ballot_sync(~0u, nt > 0));
+    if (tiles == 0) return;
+    choose(tiles, used, most);
     const int places = nt ? (nt + lead_places(nt, whole_run)) * hc_count : 0;
+    if (!partition(__reduce_add_sync(~0u, places))) return;
     int end = places;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int up = __shfl_up_sync(~0u, end, o);
       if (lane >= o) end += up;
     }
-    const int seq = __ffs(__ballot_sync(~0u, wx0 < end)) - 1;   // (wx0 < x1 unless the part is empty: then -1 or any)
-    const int n_seq = __shfl_sync(~0u, n, seq & 31), begin = __shfl_sync(~0u, end - places, seq & 31);
-    if (wx0 < wx1 && seq >= 0) open_at(seq, n_seq, wx0, begin);
-    else wx1 = wx0;
+    if (whole_run) {   // one head: its empty places are nobody's
+      const int seq = __ffs(__ballot_sync(~0u, x0 < end)) - 1, begin = __shfl_sync(~0u, end - places, seq);
+      open_at(seq, __shfl_sync(~0u, n, seq), x0, begin);
+      if (cur.at < cur.lead) {
+        cur.x += cur.lead - cur.at;
+        cur.at = cur.lead;
+      }
+      share_out(cur.x);
+      cur.at += wx0 - cur.x;
+      cur.x = wx0;
+    } else {
+      share_out(x0);
+      const int seq = __ffs(__ballot_sync(~0u, wx0 < end)) - 1;   // (wx0 < x1 unless the part is empty: then -1 or any)
+      const int n_seq = __shfl_sync(~0u, n, seq & 31), begin = __shfl_sync(~0u, end - places, seq & 31);
+      if (wx0 < wx1 && seq >= 0) open_at(seq, n_seq, wx0, begin);
+      else wx1 = wx0;
+    }
   } else {
     if (tid == 0) s_empty = 0;
     __syncthreads();
-    int tiles = 0, used = 0, filled = 0;
+    int tiles = 0, used = 0, most = 0;
 #pragma unroll 1
     for (int base = 0; base < a.n_seqs; base += kThreads) {
       const int s = base + tid;
@@ -281,15 +318,15 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
       const int nt = tile_count<TT>(a, n);
       tiles += nt;
       used += nt > 0;
-      filled += (nt + kWarps - 1) / kWarps * kWarps;
+      most = nt > most ? nt : most;
     }
     tiles = __reduce_add_sync(~0u, tiles);
     used = __reduce_add_sync(~0u, used);
-    filled = __reduce_add_sync(~0u, filled);
+    most = __reduce_max_sync(~0u, most);
     if (lane == 0) {
       s_scan[warp] = tiles;
       s_sums[0][warp] = used;
-      s_sums[1][warp] = filled;
+      s_sums[1][warp] = most;
     }
     __syncthreads();
     if (s_empty) {
@@ -297,14 +334,32 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
       for (int s = cta; s < a.n_seqs; s += grid)
         if (__ldcg(a.len + s) <= 0) zeros(s);
     }
-    tiles = used = filled = 0;
+    tiles = used = most = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       tiles += s_scan[w];
       used += s_sums[0][w];
-      filled += s_sums[1][w];
+      most = s_sums[1][w] > most ? s_sums[1][w] : most;
     }
-    if (tiles == 0 || !partition(tiles, used, filled)) return;
+    if (tiles == 0) return;
+    choose(tiles, used, most);
+    int total = (tiles + used * kToll) * hc_count;
+    if (whole_run) {
+      total = 0;
+#pragma unroll 1
+      for (int s = tid; s < a.n_seqs; s += kThreads) {
+        const int nt = tile_count<TT>(a, clamp_len(a, __ldcg(a.len + s)));
+        total += nt ? (nt + lead_places(nt, whole_run)) * hc_count : 0;
+      }
+      total = __reduce_add_sync(~0u, total);
+      __syncthreads();
+      if (lane == 0) s_scan[warp] = total;
+      __syncthreads();
+      total = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) total += s_scan[w];
+    }
+    if (!partition(total)) return;
     // sequence that x0 lies in
 #pragma unroll 1
     for (int at = 0;; chunk_base += kThreads) {
@@ -337,6 +392,7 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
       __syncthreads();
       if (x0 < at + chunk) {
         open_at(chunk_base + s_last, s_len[s_last], x0, s_scan[kWarps]);
+        share_out(whole_run && cur.at < cur.lead ? x0 - cur.at + cur.lead : x0);   // (one head: its empty places are nobody's)
         break;
       }
       at += chunk;
@@ -993,15 +1049,17 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, c
   a.chunks = (a.group + S::HEADS - 1) / S::HEADS;
   const int span = a.window > 0 && a.window < a.max_len ? a.window + S::TT : a.max_len;
   const long long each = (static_cast<long long>(span) + S::TT - 1) / S::TT;   // tiles of a head, as many as there can be
-  const long long per_seq = ((each + S::WARPS - 1) / S::WARPS * S::WARPS + kToll) * a.heads * a.chunks;
-  if (per_seq > 0x3fffffff) return VQ_ERR_UNSUPPORTED;
+  // (places: a head's tiles and kToll, or up to twice its tiles and a run of kWarps filled up - then for one head per CTA at most)
+  const long long per_seq = (each + kToll) * a.heads * a.chunks;
+  if (per_seq > 0x3fffffff || 2 * each + S::WARPS > 0x3fffffff / kMaxCtas) return VQ_ERR_UNSUPPORTED;
   // as many sequences at a time as have places below 2^30 (tens of terabytes of cache: one launch is what there is)
   const long long seqs = 0x3fffffff / per_seq;
   for (long long from = 0, all = a.n_seqs; from < all; from += seqs) {
     a.n_seqs = static_cast<int>(all - from < seqs ? all - from : seqs);
-    const long long most = per_seq * a.n_seqs / S::WARPS;
+    const long long most = (each + S::WARPS - 1) / S::WARPS * a.heads * a.chunks * a.n_seqs;   // runs of kWarps tiles
     long long ctas = sms < kMaxCtas ? sms : kMaxCtas;
     if (ctas > most) ctas = most;
+    a.inv_grid = 1.0f / static_cast<float>(ctas);
     const vq_status st = launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(S::THREADS), S::SMEM, s, a, maps[0], maps[1]);
     if (st != VQ_OK) return st;
     a.len += a.n_seqs;
