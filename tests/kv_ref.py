@@ -8,17 +8,14 @@ import torch
 
 def cache_rows(pool, scale, table_row, head, tokens, page_tokens, n_pages):
     """Keys (or values) of the listed tokens of one head in 64 bits, and which of them lie on a page of the pool."""
-    rows, ok = [], []
-    for t in tokens:
-        page = int(table_row[t // page_tokens])
-        good = 0 <= page < n_pages
-        ok.append(good)
-        if not good:
-            rows.append(torch.zeros(pool.shape[-1], dtype=torch.float64))
-            continue
-        x = pool[page, head, t % page_tokens].double()
-        rows.append(x if scale is None else x * scale[page, head, t % page_tokens].double())
-    return torch.stack(rows) if rows else torch.zeros(0, pool.shape[-1], dtype=torch.float64), ok
+    at = torch.tensor(list(tokens), dtype=torch.int64)
+    page = table_row[at // page_tokens].long()
+    ok = (page >= 0) & (page < n_pages)
+    page = torch.where(ok, page, torch.zeros_like(page))
+    x = pool[page, head, at % page_tokens].double()
+    if scale is not None:
+        x = x * scale[page, head, at % page_tokens].double()[:, None]
+    return x, ok
 
 
 def attention(q, k, v, ks, vs, table, lens, page_tokens, scale, window):
@@ -36,8 +33,7 @@ def attention(q, k, v, ks, vs, table, lens, page_tokens, scale, window):
         for h in range(hk):
             kk, ok = cache_rows(k, ks, table[s], h, tokens, page_tokens, n_pages)
             vv, _ = cache_rows(v, vs, table[s], h, tokens, page_tokens, n_pages)
-            keep = torch.tensor(ok, dtype=torch.bool)
-            kk, vv = kk[keep], vv[keep]
+            kk, vv = kk[ok], vv[ok]
             if not len(kk):
                 continue
             for i in range(h * (hq // hk), (h + 1) * (hq // hk)):

@@ -142,6 +142,28 @@ def test_attention_splits(lens, int8):
     check(c, q, *attend(c, q, 0.125), 0.125)
 
 
+def _rng_lens(seed, n, lo, hi):
+    return [int(x) for x in np.random.default_rng(seed).integers(lo, hi + 1, n)]
+
+
+# How the heads are shared out over CTAs: a CTA each; an equal number of CTAs each; runs of whole heads; runs that cut heads;
+# each with the sequences found by warps (up to 32) and by the CTA, over more sequences than it holds at a time.
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lens,heads,group,dim,page", [
+    ([900, 17, 0, 333, 512], 8, 4, 128, 16), ([700] * 40, 2, 3, 64, 32), (_rng_lens(1, 60, 0, 700), 1, 2, 80, 8),
+    ([6000, 4000, 5], 2, 8, 64, 64), ([3000] * 35, 1, 2, 64, 16), (_rng_lens(2, 50, 1, 4000), 1, 2, 64, 32), ([2500, 2500], 8, 10, 128, 16),
+    (_rng_lens(3, 20, 60, 330), 8, 4, 128, 16), (_rng_lens(4, 32, 0, 250), 8, 9, 96, 8), (_rng_lens(5, 300, 0, 200), 2, 2, 64, 8), (_rng_lens(6, 1000, 0, 260), 1, 2, 64, 16),
+    (_rng_lens(7, 30, 0, 1400), 8, 2, 64, 32), (_rng_lens(8, 5, 600, 1500), 32, 1, 64, 16), (_rng_lens(9, 500, 0, 1100), 1, 3, 64, 32), (_rng_lens(10, 900, 0, 40), 1, 1, 256, 8),
+    ([0] * 400 + [70] + [0] * 500 + [3000], 1, 2, 64, 16), (_rng_lens(11, 2000, 0, 120), 1, 1, 64, 16),
+])
+def test_attention_shared_out(lens, heads, group, dim, page, int8):
+    c = Cache(lens, heads, dim, page, int8, seed=len(lens) + heads, poison=sum(lens) < 60000)
+    q = queries(len(lens), heads * group, dim, 19)
+    check(c, q, *attend(c, q, dim ** -0.5), dim ** -0.5)
+    if len(lens) < 100:
+        check(c, q, *attend(c, q, dim ** -0.5, 200), dim ** -0.5, 200)
+
+
 def test_attention_many_short():
     rng = np.random.default_rng(3)
     lens = [int(n) for n in rng.integers(0, 40, 700)]
