@@ -227,13 +227,15 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       return;
     }
     __syncthreads();
+    int page_ahead = tid < total ? l.dst[tid] : 0;
 #pragma unroll 1
     for (int r = tid; r < total; r += kBookThreads) {
+      const int page = page_ahead;
+      if (r + kBookThreads < total) page_ahead = l.dst[r + kBookThreads];
       int lo = 0;   // last thread whose sequences' share begins at or in front of r
 #pragma unroll
       for (int step = kBookThreads / 2; step; step >>= 1)
         if (s_first[lo + step] <= r) lo += step;
-      const int page = l.dst[r];
       int s = lo * per, at = r - s_first[lo], there = s_have[lo];
       if (per > 1) {   // a thread's sequences one by one
         Share h = share_of(s);
@@ -318,7 +320,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
 }
 
 // ---- vq_kv_free ---------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) free_kernel(KvGeometry g, KvBooks b, int* refs, const int* slots, int n_slots) {
+__global__ void __launch_bounds__(kBookThreads) free_kernel(KvGeometry g, KvBooks b, int* refs, const int* slots, int n_slots) {
   pdl_launch_dependents();
   pdl_wait();
   const int i = blockIdx.x;   // a CTA per entry
@@ -329,9 +331,13 @@ __global__ void __launch_bounds__(256) free_kernel(KvGeometry g, KvBooks b, int*
   __syncthreads();
   const int pages = (s_len + g.page_tokens - 1) >> g.page_shift;
   const int* row = b.table + static_cast<long long>(seq) * b.table_stride;
-  for (int j = threadIdx.x; j < pages; j += blockDim.x) {
-    const int page = __ldcg(row + j);
-    if (static_cast<unsigned>(page) < static_cast<unsigned>(g.n_pages)) atomicSub(refs + page, 1);
+  for (int j0 = threadIdx.x; j0 < pages; j0 += 4 * blockDim.x) {
+    int page[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) page[k] = j0 + k * static_cast<int>(blockDim.x) < pages ? __ldcg(row + j0 + k * blockDim.x) : -1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (static_cast<unsigned>(page[k]) < static_cast<unsigned>(g.n_pages)) atomicSub(refs + page[k], 1);
   }
 }
 
@@ -525,7 +531,8 @@ vq_status launch_kv_fork(const KvGeometry& g, const KvPools& pools, const KvBook
 }
 
 vq_status launch_kv_free(const KvGeometry& g, const KvBooks& books, int* refs, const int* slots, int n_slots, cudaStream_t s) {
-  return launch_dependent(free_kernel, dim3(static_cast<unsigned>(n_slots)), dim3(256), 0, s, g, books, refs, slots, n_slots);
+  return launch_dependent(free_kernel, dim3(static_cast<unsigned>(n_slots)), dim3(books.table_stride > 1024 ? kBookThreads : 256), 0, s, g, books,
+                          refs, slots, n_slots);
 }
 
 vq_status launch_kv_compact(const KvGeometry& g, const KvPools& pools, const KvBooks& books, int* refs, int* status, void* ws,
