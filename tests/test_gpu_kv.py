@@ -548,6 +548,23 @@ def test_books_large():
     d.reserve([0, 64 * 12 + 1, 0, 0])               # one row too short
 
 
+def test_books_beyond_a_span():
+    """More pages than are counted at a time (65,536), pages taken and moved across the borders."""
+    d = DeviceBooks(kv_ref.Books(140001, 8, 120, 2600), 1, 1, 16, True, seed=6)
+    rng = np.random.default_rng(6)
+    d.reserve([8 * 1130 - i % 8 for i in range(120)])     # 135,600 pages
+    assert max(p for p, r in enumerate(d.m.refs) if r) > 2 * 65536
+    d.free([int(x) for x in rng.permutation(120)[:50]])
+    empty = [s for s in range(120) if d.m.len[s] == 0]
+    live = [s for s in range(120) if d.m.len[s]]
+    d.fork([[live[i], e] for i, e in enumerate(empty[:30])])
+    d.free(live[:20])
+    d.compact()
+    d.reserve([int(x) for x in rng.integers(0, 4000, 120)])
+    d.reserve([20000] * 120)     # not enough, whatever the row
+    d.compact()
+
+
 def test_fork_many_entries_and_free_repeated():
     d = DeviceBooks(kv_ref.Books(3000, 8, 1100, 10), 1, 1, 16, True, seed=3)
     d.reserve([20, 0, 16] + [0] * 1097)
@@ -598,7 +615,9 @@ def norm_ref(x, layer, w, b, eps):
 @pytest.mark.parametrize("layer,post,gate,wide", [
     (False, False, 0, False), (True, True, 1, True), (False, True, 2, False), (True, False, 2, True), (False, True, 1, True), (True, True, 0, False),
 ])
-@pytest.mark.parametrize("n_rows,n_cols", [(1, 1), (3, 7), (5, 8), (9, 100), (2, 256), (7, 257), (3, 264), (1, 4096), (4, 4100), (300, 512), (2, 8192), (150, 1000), (2, 32768), (1, 32767)])
+@pytest.mark.parametrize("n_rows,n_cols", [(1, 1), (3, 7), (5, 8), (9, 100), (2, 256), (7, 257), (3, 264), (1, 4096), (4, 4100), (300, 512), (2, 8192), (150, 1000), (2, 32768), (1, 32767),
+                                           # many rows: a warp each, rings of rows (with a gate per element one CTA an SM), odd widths
+                                           (300, 520), (301, 700), (310, 1000), (600, 1032), (400, 4096), (310, 8192), (300, 16384), (300, 257), (310, 1001), (300, 16385)])
 def test_norm(n_rows, n_cols, layer, post, gate, wide):
     rng = np.random.default_rng(n_rows * 1000 + n_cols)
     half = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float16))  # noqa: E731
@@ -670,6 +689,22 @@ def test_norm_parts_and_places(n_cols):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(x2, out) and torch.equal(y2, h)
+
+
+@pytest.mark.parametrize("n_rows,n_cols,wide", [(700, 4096, True), (700, 2048, False), (2000, 600, True), (310, 16384, False)])
+def test_norm_in_place_many_rows(n_rows, n_cols, wide):
+    """x' over x and h over y while other rows are under way: as with outputs of their own."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n_rows)
+    draw_ = lambda *s: torch.randn(s, generator=g, device=DEV).half()  # noqa: E731
+    x, y, w, pw = draw_(n_rows, n_cols), draw_(n_rows, n_cols), draw_(n_cols), draw_(n_cols)
+    x = x.float() if wide else x
+    nb = vq.VQNorm(n_rows, n_cols, vq.VQ_NORM_LAYER, int(wide), vq.VQ_GATE_NONE, 1e-5, 0.5, n_cols, n_cols, 0, n_cols, n_cols)
+    out, h = torch.empty_like(x), torch.empty_like(y)
+    vq.vq_residual_norm(nb, x, y, None, pw, None, w, None, out, h)
+    vq.vq_residual_norm(nb, x, y, None, pw, None, w, None, x, y)
+    torch.cuda.synchronize()
+    assert torch.equal(x, out) and torch.equal(y, h)
 
 
 # ---- a decode step ---------------------------------------------------------------------------------------------------------
@@ -762,3 +797,8 @@ def test_decode_steps_of_a_block():
         assert float((h.cpu().double() - ref)[on].abs().max()) < 0.02 * float(ref[on].abs().max())
     assert length.cpu().tolist() == [12, 0, 12]
     assert sorted(p for p, r in enumerate(refs.cpu().tolist()) if r) == list(range(sum(1 for r in refs.cpu().tolist() if r)))
+
+
+def test_no_wait_ran_out():
+    """Every bounded wait of the kernels above found its copy."""
+    assert vq.vq_device_wait_failures() == 0

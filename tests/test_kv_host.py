@@ -187,6 +187,37 @@ def test_host_tensors_are_refused():
         vq.vq_residual_norm(NORM, t, t, None, None, None, t, None, t, t)
 
 
+def test_handles_check_their_tensors():
+    torch = pytest.importorskip("torch")
+    half, i8, f32, i32 = (torch.zeros(64, dtype=t) for t in (torch.float16, torch.int8, torch.float32, torch.int32))
+    for bad in ((f32, f32), (half, i8), (i8, i8), (i8, i8, half, half), (half, half, f32, f32), (half[::2], half[::2])):
+        with pytest.raises(ValueError, match="KVPool"):
+            vq.KVPool(*bad)
+    for bad in ((i32.long().view(8, 8), i32[:8]), (i32.view(8, 8), f32[:8]), (i32.view(8, 8), i32[:7]), (i32.view(8, 8)[:, 2:], i32[:8]), (i32, i32)):
+        with pytest.raises(ValueError, match="KVSeqs"):
+            vq.KVSeqs(*bad)
+    with pytest.raises(ValueError, match="KVRotary"):
+        vq.KVRotary(f32, 5, 16, 0)
+    with pytest.raises(ValueError, match="KVRotary"):
+        vq.KVRotary(half, 4, 16, 0)
+    small = vq.VQKVFormat(2, 8, 1, 16, vq.VQ_KV_FP16)
+    full, short, bytes_ = (torch.zeros(n, dtype=t) for n, t in ((256, torch.float16), (255, torch.float16), (256, torch.int8)))
+    binding._room(vq.KVPool(full, full), small)
+    for k, v, ks, vs in ((short, full, None, None), (full, short, None, None), (bytes_, bytes_, f32[:15], f32[:16])):
+        with pytest.raises(ValueError, match="smaller"):
+            binding._room(vq.KVPool(k, v, ks, vs), small)
+
+
+def test_handles_copied():
+    """A copy's struct is its own: its address outlives the original."""
+    import copy
+    import pickle
+    for h in (GOOD, NORM):
+        for c in (copy.copy(h), copy.deepcopy(h), pickle.loads(pickle.dumps(h))):
+            assert c == h and hash(c) == hash(h) and c._p == ctypes.addressof(c._c) and c._p != h._p
+            assert bytes(c._c) == bytes(h._c)
+
+
 def test_books_follow_the_rules():
     """The model that the GPU tests compare with, on a case worked out by hand."""
     b = Books(8, 8, 4, 4)
