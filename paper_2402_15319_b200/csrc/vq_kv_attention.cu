@@ -31,10 +31,10 @@ using namespace dev;
 constexpr int kToll = 2;                // places in front of a head's tiles: what beginning and ending one costs, in tiles
 constexpr int kWaitTries = 1 << 18;     // mbarrier polls before a warp gives up and flags an error
 constexpr int kMaxHeads = 16;           // query heads that a CTA takes together at most
-constexpr int kMaxCtas = 256;          // CTAs of a launch, one per SM (partial sums and counters are sized for them)
+constexpr int kMaxCtas = 256;           // CTAs of a launch, one per SM (partial sums and counters are sized for them)
 constexpr int kMaxWarps = 12;
-// Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, and two binary16 pieces hold a weight of
-// 2^-18 of the largest to 2^-32 of it.
+// Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, weights down to 2^-21 of the largest are normal
+// numbers, and the two binary16 pieces of any weight together are off by 2^-32 of the largest at most.
 constexpr float kLift = 7.0f, kSlack = 8.0f;
 
 struct AttnArgs {
@@ -245,7 +245,8 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
     if (whole_cost <= run_cost) whole_run = most;
     if (whole_cost <= kWarps + S::JOIN_COST && whole_run) return;
     int each = static_cast<int>(__fdividef(static_cast<float>(grid), static_cast<float>(heads)));   // (heads * each <= grid)
-    if (heads * each > grid) --each;
+    each = heads * each > grid ? each - 1 : each;
+    each = each < 1 ? 1 : each;
     const int per = static_cast<int>(__fdividef(static_cast<float>(most), static_cast<float>(each))) + 1;
     const int part = per > kWarps ? per : kWarps;
     const float part_cost = part + S::JOIN_COST;
@@ -1078,7 +1079,7 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, c
   a.chunks = (a.group + S::HEADS - 1) / S::HEADS;
   const int span = a.window > 0 && a.window < a.max_len ? a.window + S::TT : a.max_len;
   const long long each = (static_cast<long long>(span) + S::TT - 1) / S::TT;   // tiles of a head, as many as there can be
-  // (places: a head's tiles and kToll, or up to twice its tiles and a run of kWarps filled up - then for one head per CTA at most)
+  // (places: a head's tiles and kToll, or a run of its longest head's tiles for each CTA)
   const long long per_seq = (each + kToll) * a.heads * a.chunks;
   if (per_seq > 0x3fffffff || 2 * each + S::WARPS > 0x3fffffff / kMaxCtas) return VQ_ERR_UNSUPPORTED;
   // as many sequences at a time as have places below 2^30 (tens of terabytes of cache: one launch is what there is)

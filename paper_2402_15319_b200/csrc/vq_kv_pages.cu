@@ -1,10 +1,10 @@
 // The cache's books and the pages they move: vq_kv_reserve, vq_kv_fork, vq_kv_free, vq_kv_compact, vq_kv_copy_pages.
 //
 // Books are whole numbers on the device.  What depends on order - which free page a sequence gets - is decided by one CTA.
-// It gets the reference counts as bits: a cluster of eight CTAs reads them (one SM alone draws 16 bytes a clock from L2:
+// It gets the reference counts as bits: a cluster of eight CTAs reads them (one SM alone drew 16 bytes a clock from L2:
 // 65,536 pages took 8.5 us), ballots make words of them that go to the first CTA's shared memory, and scans of the words'
-// counts rank the pages, so equal books give equal books.  What does not depend on order - page data, table rows, counts of shared pages - is left to a second kernel on the whole GPU, which finds the list of
-// pages in the workspace.
+// counts rank the pages, so equal books give equal books.  What does not depend on order - page data, table rows, counts
+// of shared pages - is left to a second kernel on the whole GPU, which finds the list of pages in the workspace.
 // Counting 65,536 pages and entering 1750 for 256 sequences: 7.8 us; moving 980 pages of 32 KB in 8 layers: 174 us = 5.9 TB/s.
 #include "vq_device.cuh"
 #include "vq_kv.cuh"
