@@ -4,7 +4,7 @@
 // stays in registers between its reductions (pieces of eight columns, PER of them a thread), the mean and the centred
 // squares are summed one after the other, in binary32, in a fixed order.
 // 8192 x 8192, both norms, gate per channel, binary32 residual: 143 us = 5.6 TB/s (with rows straight into registers and weights
-// past L1 207); one row of 4096: 2.0 us.
+// past L1 207); one row of 4096: 1.9 us.
 #include "vq_device.cuh"
 #include "vq_kv.cuh"
 #include "vq_residual_norm.cuh"
@@ -115,11 +115,23 @@ __device__ __forceinline__ float row_sum(float v, RowSums& r) {
 }
 
 // The norm of the row in `u`: mean taken away (layer), divided by the root of the mean square; weights and biases follow.
-// CACHED: they may come through L1.
-template <bool VEC, bool WARP_ROW, int PER, bool CACHED>
+// CACHED: they may come through L1.  EARLY 1: weights asked for before the sums, 2: biases too, where registers hold them (8192
+// rows of 4096, rings: 77 -> 70 us, with LayerNorm's 94 -> 97; 16384 of 1000, a warp each: 47 -> 43; one of 4096: 2.02 -> 1.95;
+// with rings of 8192 columns, 512 threads: 142 -> 144, so not there, nor with 1024 threads: 200 rows of 8192 6.9 -> 8.4).
+template <bool VEC, bool WARP_ROW, int PER, bool CACHED, int EARLY>
 __device__ __forceinline__ void norm(Float8 (&u)[PER], const __half* weight, const __half* bias, const ResidualNorm& a, int first, int step,
                                      RowSums& s) {
   const float inv_n = 1.0f / static_cast<float>(a.cols);
+  uint4 w8[PER], b8[PER];
+  if (VEC && EARLY) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = piece<VEC>(first, step, i);
+      w8[i] = b8[i] = make_uint4(0, 0, 0, 0);
+      if (c < a.cols) w8[i] = fetch_global<uint4, CACHED>(reinterpret_cast<const uint4*>(weight + c));
+      if (EARLY == 2 && c < a.cols && bias) b8[i] = fetch_global<uint4, CACHED>(reinterpret_cast<const uint4*>(bias + c));
+    }
+  }
   if (a.layer) {
     float sum = 0.0f;
 #pragma unroll
@@ -142,9 +154,10 @@ __device__ __forceinline__ void norm(Float8 (&u)[PER], const __half* weight, con
   for (int i = 0; i < PER; ++i) {
     const int c = piece<VEC>(first, step, i);
     if (c >= a.cols) continue;
-    const Float8 w = load8h<VEC, CACHED>(weight, c, a.cols, step);
+    const Float8 w = VEC && EARLY ? unpack8(w8[i]) : load8h<VEC, CACHED>(weight, c, a.cols, step);
     Float8 b = {};
-    if (bias) b = load8h<VEC, CACHED>(bias, c, a.cols, step);
+    if (VEC && EARLY == 2) b = unpack8(b8[i]);
+    else if (bias) b = load8h<VEC, CACHED>(bias, c, a.cols, step);
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[i].v[e] = u[i].v[e] * r * w.v[e] + b.v[e];
   }
@@ -155,6 +168,7 @@ template <bool VEC, bool WIDE, bool WARP_ROW, int PER, int MAX_THREADS, bool CAC
 __global__ void __launch_bounds__(MAX_THREADS) residual_norm_kernel(ResidualNorm a) {
   __shared__ float s_sums[64];
   RowSums s = {s_sums, 0};
+  constexpr int kEarly = WARP_ROW || (PER == 1 && MAX_THREADS <= 512) ? 2 : 0;
   if (!CACHED) {
     pdl_launch_dependents();
     pdl_wait();
@@ -181,7 +195,7 @@ __global__ void __launch_bounds__(MAX_THREADS) residual_norm_kernel(ResidualNorm
       y[i] = {};
       if (c < a.cols) y[i] = load8h<VEC>(yr, c, a.cols, step);
     }
-    if (a.post_w) norm<VEC, WARP_ROW, PER, CACHED>(y, a.post_w, a.post_b, a, first, step, s);
+    if (a.post_w) norm<VEC, WARP_ROW, PER, CACHED, kEarly>(y, a.post_w, a.post_b, a, first, step, s);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = piece<VEC>(first, step, i);
@@ -207,7 +221,7 @@ __global__ void __launch_bounds__(MAX_THREADS) residual_norm_kernel(ResidualNorm
     }
   }
   if (a.h) {
-    norm<VEC, WARP_ROW, PER, CACHED>(x, a.pre_w, a.pre_b, a, first, step, s);
+    norm<VEC, WARP_ROW, PER, CACHED, kEarly>(x, a.pre_w, a.pre_b, a, first, step, s);
     __half* hr = a.h + row * a.h_stride;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -282,7 +296,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) residual_norm_rows_ke
       phase ^= 1;
     }
     if (a.y) {
-      if (a.post_w) norm<true, false, PER, true>(y, a.post_w, a.post_b, a, tid, THREADS, s);
+      if (a.post_w) norm<true, false, PER, true, (THREADS <= 256)>(y, a.post_w, a.post_b, a, tid, THREADS, s);
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         if (a.gate) {
@@ -303,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) residual_norm_rows_ke
       }
     }
     if (a.h) {
-      norm<true, false, PER, true>(x, a.pre_w, a.pre_b, a, tid, THREADS, s);
+      norm<true, false, PER, true, (THREADS <= 256)>(x, a.pre_w, a.pre_b, a, tid, THREADS, s);
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int c = (tid + i * THREADS) * 8;
@@ -364,6 +378,7 @@ vq_status launch(const ResidualNorm& a, int sms, cudaStream_t s) {
   }
   // A row per CTA, as many threads as it has pieces while they suffice: the shortest way through the row.
   auto threads = [&](int per) { return ((pieces + per - 1) / per + 31) / 32 * 32; };
+  if (pieces <= 512 && !many) return launch_one<VEC, WIDE, false, 1, 512>(a, threads(1), many, s);
   if (pieces <= 1024 && !many) return launch_one<VEC, WIDE, false, 1, 1024>(a, threads(1), many, s);
   if (pieces <= 1024) return launch_one<VEC, WIDE, false, 2, 512>(a, threads(2), many, s);
   return launch_one<VEC, WIDE, false, 4, 1024>(a, threads(4), many, s);
