@@ -428,8 +428,9 @@ typedef struct {
  *              a sequence of length 0 takes none).
  *   d_k, d_v : device binary16 [n_tokens] rows of n_kv_heads * head_dim, k_stride / v_stride elements apart.
  * Rotation is binary32, rounded once.  VQ_KV_INT8 stores, per token and head, scale = max|x| / 127 and the integers
- * nearest x * (1 / scale) (ties to even) of the rotated, not yet rounded x; a row of zeros has scale 0; one that
- * holds an infinity or NaN reads back as no number.  Strides: multiples of 8.
+ * nearest 127 x / max|x| (ties to even; one rounded quotient) of the rotated, not yet rounded x; a row of zeros has
+ * scale 0, one below 2^-118 throughout reads back as zeros, one that holds an infinity or NaN as no number.  Strides:
+ * multiples of 8.
  * Errors: NULL, FORMAT, SHAPE, ALIGN, CUDA. */
 vq_status vq_kv_append(const vq_kv_format* fmt, const vq_kv_pool* pool, const vq_kv_seqs* seqs, const void* d_starts, int n_tokens,
                        const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride, const vq_kv_rotary* rotary, void* stream);

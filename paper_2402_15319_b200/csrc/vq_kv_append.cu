@@ -1,6 +1,6 @@
 // New tokens into the paged cache (vq_kv_append): queries and keys rotated, keys and values written to their pages.
 //
-//   (a, b) -> (a cos - b sin, b cos + a sin),   8-bit rows: scale = max|x| / 127, integer = rint(x / scale).
+//   (a, b) -> (a cos - b sin, b cos + a sin),   8-bit rows: scale = max|x| / 127, integer = rint(127 x / max|x|).
 //
 // Bound by memory: every row is read once and written once.  A CTA serves one token, or (few tokens) a share of one's heads,
 // so the token's cosines and sines are fetched once per thread and used for all of them.  A group of LG lanes holds a head's row:
@@ -171,16 +171,21 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
 #pragma unroll
       for (int o = LG / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
       if (mine && kv >= 0 && on_page) {
-        const float scale = __fdiv_rn(__uint_as_float(top), 127.0f);
+        const float most = __uint_as_float(top), scale = __fdiv_rn(most, 127.0f);
         uint32_t w[4] = {0, 0, 0, 0};
-        const float inv = __fdiv_rn(1.0f, scale);
-        if (scale > 0.0f) {
+        if (most >= 0x1p-118f) {   // (below that, which no binary16 row is but by a table of such cosines, the reciprocal ends: zeros)
+          // 127 / 128 x of a binary16 value is exact in binary32, and the quotient is rounded once (a rounded reciprocal, then one
+          // step with the exact remainder: Markstein's theorem), so a row that is not rotated gets the nearest integers always,
+          // ties (one value in 2000) to even.  x / scale by the rounded reciprocal alone was one off in 1.1e-4 of them.
+          const float whole = most * 0.0078125f, inv = __frcp_rn(whole);
+          auto nearest = [&](float v) {   // low byte: between -127 and 127, as |v| <= most; 1.5 * 2^23 leaves no place behind the point
+            const float part = v * 0.9921875f, q = part * inv;
+            return __float_as_uint(fmaf(fmaf(-q, whole, part), inv, q) + 12582912.0f);
+          };
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int u = max(-127, min(127, __float2int_rn(x[i] * inv)));
-            const int r = max(-127, min(127, __float2int_rn(y[i] * inv)));
-            w[i / 4] |= static_cast<uint32_t>(u & 255) << (8 * (i % 4));
-            w[2 + i / 4] |= static_cast<uint32_t>(r & 255) << (8 * (i % 4));
+          for (int i = 0; i < 2; ++i) {
+            w[i] = prmt(prmt(nearest(x[4 * i]), nearest(x[4 * i + 1]), 0x0040), prmt(nearest(x[4 * i + 2]), nearest(x[4 * i + 3]), 0x0040), 0x5410);
+            w[2 + i] = prmt(prmt(nearest(y[4 * i]), nearest(y[4 * i + 1]), 0x0040), prmt(nearest(y[4 * i + 2]), nearest(y[4 * i + 3]), 0x0040), 0x5410);
           }
         }
         uint8_t* dst = (value ? a.pool.v : a.pool.k) + at * a.g.dim;

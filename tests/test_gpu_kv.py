@@ -441,6 +441,26 @@ def test_append_int8_odd_rows():
     assert torch.allclose(got[3], k[3, 0].double(), rtol=2.0 ** -20, atol=0) and torch.allclose(got[4], k[4, 0].double(), rtol=2.0 ** -20, atol=0)
 
 
+@pytest.mark.parametrize("dim,heads,tokens", [(16, 3, 700), (80, 2, 700), (128, 8, 5000), (256, 2, 900)])
+def test_append_int8_nearest_integers(dim, heads, tokens):
+    """Rows that are not rotated: the integers are those nearest 127 x / max|x| in whole-number arithmetic, ties to even (about
+    one value in 2000 of such rows is one), the scale is max|x| / 127 rounded once."""
+    page = 16
+    c = Cache([tokens], heads, dim, page, True, seed=dim, poison=False)
+    new = [rows(tokens, heads, dim, 31), rows(tokens, heads, dim, 32)]
+    (k2, v2, ks2, vs2), _ = run_append(c, [0, tokens], *new, None, None, 0, 0)
+    at = torch.arange(tokens)
+    where, slot = c.table[0, at // page].long(), at % page
+    for x, got, scale in ((new[0], k2, ks2), (new[1], v2, vs2)):
+        whole = (x.double() * 2.0 ** 24).long()      # binary16 values are multiples of 2^-24, below 2^40 of them
+        top = whole.abs().amax(-1, keepdim=True)
+        double = 254 * whole + top                   # 2 top (127 x / top + 1/2)
+        want = torch.div(double, 2 * top, rounding_mode="floor")
+        want = want - ((double % (2 * top) == 0) & (want % 2 != 0)).long()
+        assert torch.equal(got[where, :, slot].long(), want), f"{int((got[where, :, slot].long() != want).sum())} of {want.numel()} off"
+        assert np.array_equal(scale[where, :, slot].numpy(), x.float().abs().amax(-1).numpy() / np.float32(127))
+
+
 # ---- pages ----------------------------------------------------------------------------------------------------------
 
 class DeviceBooks:
