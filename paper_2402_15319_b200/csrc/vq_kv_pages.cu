@@ -83,8 +83,9 @@ struct PageBits {
     return above & below;
   }
 };
-// By all CTAs of the cluster: each reads an eighth, the words meet in CTA 0's `s_words`, and CTA 0 gets its bits.  Between two
-// calls CTA 0 has to be done with the words: next_span().
+// By all CTAs of the cluster: each reads an eighth, the words meet in CTA 0's `s_words`, and CTA 0 gets its bits.  A store into
+// CTA 0's shared memory has to come behind its start, and between two calls behind its use of the words before: every call waits
+// in front of its stores (the loads are under way) for an arrival of all CTAs, the kernel's first statement or next_span().
 constexpr int kBookCtas = 8;
 __device__ __forceinline__ PageBits page_bits(const int* refs, int n_pages, int base, unsigned* s_words) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = static_cast<int>(cluster_ctarank());
@@ -98,12 +99,14 @@ __device__ __forceinline__ PageBits page_bits(const int* refs, int n_pages, int 
 #pragma unroll
   for (int k = 0; k < 8; ++k) count[k] = __ldcg(refs + min(base + (word0 + k) * 32 + lane, n_pages - 1));
   const uint32_t dst = map_to_rank(smem_u32(s_words), 0);
+  __syncwarp();   // (the barrier is for whole warps)
+  cluster_wait_acquire();
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const unsigned word = __ballot_sync(~0u, count[k] != 0);
     if (lane == k && k < share / 32 && word0 + k < all) st_cluster_u32(dst + 4 * (word0 + k), word);
   }
-  __syncwarp();   // (the barrier is for whole warps)
+  __syncwarp();
   cluster_arrive_release();
   cluster_wait_acquire();
   if (rank == 0) {
@@ -116,9 +119,8 @@ __device__ __forceinline__ PageBits page_bits(const int* refs, int n_pages, int 
   return b;
 }
 __device__ __forceinline__ void next_span() {
-  __syncwarp();   // (the barrier is for whole warps)
+  __syncwarp();
   cluster_arrive_release();
-  cluster_wait_acquire();
 }
 // Numbers the set bits of w[0], w[1] over the whole CTA in the order of the pages; returns how many there are.  first[]: of
 // each word's lowest.
@@ -176,6 +178,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   __shared__ int s_first[kBookThreads];   // pages in front of a thread's sequences
   __shared__ int s_have[kBookThreads];    // pages that its first sequence has
   __shared__ unsigned s_words[kSpan / 32];
+  cluster_arrive_release();   // (page_bits waits)
   pdl_launch_dependents();
   pdl_wait();
   if (cluster_ctarank() != 0) {
@@ -266,6 +269,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   __shared__ int s_scan[32];
   __shared__ int s_child[kMaxForks];
   __shared__ unsigned s_words[kSpan / 32];
+  cluster_arrive_release();   // (page_bits waits)
   pdl_launch_dependents();
   pdl_wait();
   if (cluster_ctarank() != 0) {
@@ -346,6 +350,7 @@ __global__ void __launch_bounds__(kBookThreads) free_kernel(KvGeometry g, KvBook
 __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads) compact_kernel(KvGeometry g, KvBooks b, int* refs, int* status, void* ws) {
   __shared__ int s_scan[32];
   __shared__ unsigned s_words[kSpan / 32];
+  cluster_arrive_release();   // (page_bits waits)
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x;

@@ -232,3 +232,34 @@ def test_books_follow_the_rules():
     assert b.refs == [1, 1, 0, 2, 1, 0, 0, 0] and b.len[0] == 0
     status, copies = b.compact()
     assert status == (4, 1) and copies == [(4, 2, 8)] and b.table[1][:3] == [0, 1, 2] and b.refs == [1, 1, 1, 2, 0, 0, 0, 0]
+
+
+def test_remote_stores_wait_for_the_cluster():
+    """A CTA's shared memory may be written by another one of the cluster only after it is known to have started.  Read in the
+    source: each cluster kernel of the books arrives before anything else, and whoever stores has waited in front, in every span."""
+    import os
+    import re
+    src = open(os.path.join(vq_build.CSRC, "vq_kv_pages.cu")).read()
+    src = re.sub(r"//[^\n]*", "", src)
+
+    def body(at):
+        at = depth = src.index("{", at) + 1
+        level = 1
+        while level:
+            level += {"{": 1, "}": -1}.get(src[depth], 0)
+            depth += 1
+        return src[at:depth]
+
+    kernels = [m.end() for m in re.finditer(r"__cluster_dims__[^;{]*?\w+_kernel\(", src)]
+    assert len(kernels) == 3
+    for k in kernels:
+        b = body(k)
+        assert 0 <= b.find("cluster_arrive") < min(i for i in (b.find("page_bits("), b.find("free_pages("), b.find("return")) if i >= 0)
+        assert b.find("cluster_wait") < 0 and b.count("cluster_arrive") == 1      # (its wait is page_bits')
+    stores = [m.start() for m in re.finditer(r"st_cluster_u32\(dst", src)]
+    bits = body(src.index("PageBits page_bits("))
+    assert len(stores) == 1 and bits.count("st_cluster_u32(") == 1                # nothing else of the file stores remotely
+    order = [bits.index("cluster_wait"), bits.index("st_cluster_u32("), bits.index("cluster_arrive"), bits.rindex("cluster_wait")]
+    assert order == sorted(order) and bits.count("cluster_wait") == 2 and bits.count("cluster_arrive") == 1
+    span = body(src.index("void next_span("))
+    assert "cluster_arrive" in span and "cluster_wait" not in span                # the next page_bits waits for it
