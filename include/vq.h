@@ -399,8 +399,10 @@ vq_status vq_kv_info(const vq_kv_format* fmt, vq_kv_info_t* out);
  *               Not to be shared with the products' workspace.
  * Scores, softmax and sums are binary32; one rounding to binary16 at the end.  Masked places and what lies behind a
  * sequence's last token are not read as numbers: an infinity or NaN there changes nothing.
- * Errors: NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (head_dim; more than a launch can number: table rows of over
- * 2^25 tokens without a window, or of over 2^30 tiles of 16 tokens in all their heads, pools of 2^31 rows of keys), CUDA. */
+ * Errors: NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (head_dim; more than a launch can number: table rows, or
+ * where there is one windows, of over 2^21 tiles of 16 to 64 tokens - 2^25 tokens are never too many -, or of 2^30 tiles
+ * and more, two added each, over all key/value heads and their groups of 8 or 16 query heads; pools of 2^31 rows of
+ * keys), CUDA. */
 size_t vq_kv_attention_workspace_bytes(const vq_kv_format* fmt);
 vq_status vq_kv_attention(const vq_kv_format* fmt, const vq_kv_pool* pool, const vq_kv_seqs* seqs, int n_q_heads, const void* d_q,
                           int64_t q_stride, void* d_out, int64_t out_stride, void* d_lse, float scale, int window, void* d_ws,

@@ -1055,8 +1055,25 @@ attention_kernel(AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __
 }
 
 template <int D, bool I8, int NH>
-vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, cudaStream_t s) {
+vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, cudaStream_t s) {
   using S = Shape<D, I8, NH>;
+  // What a launch can number: rows of the pool and places of its list in 31 bits.  A list of runs that may cut heads has each head's
+  // tiles and kToll; one that gives CTAs of their own to heads (at most kMaxCtas of them then) has a run for each CTA, of up to
+  // the longest head's tiles and one, or kWarps if that is more.
+  const uint64_t dims[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(g.n_pages) * g.heads << g.page_shift};
+  a.chunks = (a.group + S::HEADS - 1) / S::HEADS;
+  const int span = a.window > 0 && a.window < a.max_len ? a.window + S::TT : a.max_len;
+  const long long each = (static_cast<long long>(span) + S::TT - 1) / S::TT;   // tiles of a head, as many as there can be
+  const long long per_seq = (each + kToll) * a.heads * a.chunks;
+  constexpr int kMostTiles = 1 << 21;
+  static_assert(static_cast<long long>(kMaxCtas) * (kMostTiles + S::WARPS) <= 0x3fffffff, "runs of a CTA each");
+  if (dims[1] > 0x7fffffffu || each > kMostTiles || per_seq > 0x3fffffff) return VQ_ERR_UNSUPPORTED;
+
+  int sms = 0;
+  vq_status st = device_sms(&sms);
+  if (st != VQ_OK) return st;
+  st = device_error_counter(&a.error_flag);
+  if (st != VQ_OK) return st;
   static int ready[kMaxDevices] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return VQ_ERR_CUDA;
@@ -1068,20 +1085,12 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, c
   // the pools as matrices of tokens; a box is a column block of the tokens that a page and a tile have in common
   while ((1 << a.run_shift) < S::TT && a.run_shift < a.page_shift) ++a.run_shift;
   CUtensorMap maps[2];
-  const uint64_t dims[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(g.n_pages) * g.heads << g.page_shift};
   const uint64_t strides[1] = {static_cast<uint64_t>(S::ROW)};
   const uint32_t box[2] = {static_cast<uint32_t>(S::CBB / (I8 ? 1 : 2)), 1u << a.run_shift};
-  if (dims[1] > 0x7fffffffu) return VQ_ERR_UNSUPPORTED;
   for (int i = 0; i < 2; ++i) {
-    const vq_status st = encode_tensor_map(&maps[i], i ? pool.v : pool.k, I8 ? 1 : 2, 2, dims, strides, box, S::CBB == 128 ? 2 : 1);
+    st = encode_tensor_map(&maps[i], i ? pool.v : pool.k, I8 ? 1 : 2, 2, dims, strides, box, S::CBB == 128 ? 2 : 1);
     if (st != VQ_OK) return st;
   }
-  a.chunks = (a.group + S::HEADS - 1) / S::HEADS;
-  const int span = a.window > 0 && a.window < a.max_len ? a.window + S::TT : a.max_len;
-  const long long each = (static_cast<long long>(span) + S::TT - 1) / S::TT;   // tiles of a head, as many as there can be
-  // (places: a head's tiles and kToll, or a run of its longest head's tiles for each CTA)
-  const long long per_seq = (each + kToll) * a.heads * a.chunks;
-  if (per_seq > 0x3fffffff || 2 * each + S::WARPS > 0x3fffffff / kMaxCtas) return VQ_ERR_UNSUPPORTED;
   // as many sequences at a time as have places below 2^30 (tens of terabytes of cache: one launch is what there is)
   const long long seqs = 0x3fffffff / per_seq;
   for (long long from = 0, all = a.n_seqs; from < all; from += seqs) {
@@ -1090,7 +1099,7 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, c
     long long ctas = sms < kMaxCtas ? sms : kMaxCtas;
     if (ctas > most) ctas = most;
     a.inv_grid = 1.0f / static_cast<float>(ctas);
-    const vq_status st = launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(S::THREADS), S::SMEM, s, a, maps[0], maps[1]);
+    st = launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(S::THREADS), S::SMEM, s, a, maps[0], maps[1]);
     if (st != VQ_OK) return st;
     a.len += a.n_seqs;
     a.table += static_cast<long long>(a.n_seqs) * a.table_stride;
@@ -1102,9 +1111,9 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, int sms, c
 }
 
 template <int D>
-vq_status launch_dim(const AttnArgs& a, const KvGeometry& g, const KvPool& pool, int sms, cudaStream_t s) {
-  if (a.group <= 8) return g.int8 ? launch<D, true, 1>(a, g, pool, sms, s) : launch<D, false, 1>(a, g, pool, sms, s);
-  return g.int8 ? launch<D, true, 2>(a, g, pool, sms, s) : launch<D, false, 2>(a, g, pool, sms, s);
+vq_status launch_dim(const AttnArgs& a, const KvGeometry& g, const KvPool& pool, cudaStream_t s) {
+  if (a.group <= 8) return g.int8 ? launch<D, true, 1>(a, g, pool, s) : launch<D, false, 1>(a, g, pool, s);
+  return g.int8 ? launch<D, true, 2>(a, g, pool, s) : launch<D, false, 2>(a, g, pool, s);
 }
 
 }  // namespace
@@ -1121,12 +1130,7 @@ size_t kv_attention_workspace_bytes(int head_dim) {
 vq_status launch_kv_attention(const KvGeometry& g, const KvPool& pool, const KvBooks& books, int n_q_heads, const __half* q,
                               long long q_stride, __half* out, long long out_stride, float* lse, float scale, int window, void* ws,
                               cudaStream_t s) {
-  int sms = 0;
-  vq_status st = device_sms(&sms);
-  if (st != VQ_OK) return st;
   AttnArgs a = {};
-  st = device_error_counter(&a.error_flag);
-  if (st != VQ_OK) return st;
   a.run_shift = 3;
   a.ks = pool.ks;
   a.vs = pool.vs;
@@ -1150,12 +1154,12 @@ vq_status launch_kv_attention(const KvGeometry& g, const KvPool& pool, const KvB
   a.window = window;
   a.scale_log2 = scale * 1.44269504088896341f;
   switch (g.dim) {
-    case 64: return launch_dim<64>(a, g, pool, sms, s);
-    case 80: return launch_dim<80>(a, g, pool, sms, s);
-    case 96: return launch_dim<96>(a, g, pool, sms, s);
-    case 128: return launch_dim<128>(a, g, pool, sms, s);
-    case 192: return launch_dim<192>(a, g, pool, sms, s);
-    case 256: return launch_dim<256>(a, g, pool, sms, s);
+    case 64: return launch_dim<64>(a, g, pool, s);
+    case 80: return launch_dim<80>(a, g, pool, s);
+    case 96: return launch_dim<96>(a, g, pool, s);
+    case 128: return launch_dim<128>(a, g, pool, s);
+    case 192: return launch_dim<192>(a, g, pool, s);
+    case 256: return launch_dim<256>(a, g, pool, s);
   }
   return VQ_ERR_UNSUPPORTED;
 }

@@ -310,6 +310,18 @@ def test_attention_offsets_beyond_32_bits(int8):
     check(c, q, out, lse, 0.1)
 
 
+@pytest.mark.parametrize("dim,int8,tokens", [(128, False, 1 << 25), (80, False, 1 << 25), (64, False, 1 << 26), (128, True, 1 << 26), (64, True, 1 << 27)])
+def test_attention_longest_rows(dim, int8, tokens):
+    """Table rows of 2^21 tiles, the most that a launch numbers: few tokens in them, with and without a window."""
+    c = Cache([700, 0, 33], 2, dim, 256, int8, seed=dim, extra_stride=0)
+    pool, _ = c.device()
+    table = torch.full((3, tokens // 256), -7, dtype=torch.int32, device=DEV)
+    table[:, :c.table.shape[1]] = c.table.to(DEV)
+    q = queries(3, 6, dim, 20)
+    for window in (0, 50):
+        check(c, q, *attend(c, q, 0.1, window, dev=(pool, vq.KVSeqs(table, c.len.to(DEV)))), 0.1, window)
+
+
 # ---- append -------------------------------------------------------------------------------------------------------
 
 def rope_table(n, rot, seed=0):

@@ -263,3 +263,22 @@ def test_remote_stores_wait_for_the_cluster():
     assert order == sorted(order) and bits.count("cluster_wait") == 2 and bits.count("cluster_arrive") == 1
     span = body(src.index("void next_span("))
     assert "cluster_arrive" in span and "cluster_wait" not in span                # the next page_bits waits for it
+
+
+@pytest.mark.parametrize("dim,kv_type,heads,tokens", [
+    (128, vq.VQ_KV_FP16, 1, 1 << 25), (80, vq.VQ_KV_FP16, 4, 1 << 25), (64, vq.VQ_KV_FP16, 1, 1 << 26), (256, vq.VQ_KV_INT8, 2, 1 << 25),
+    (128, vq.VQ_KV_INT8, 1, 1 << 26), (64, vq.VQ_KV_INT8, 1, 1 << 27),
+])
+def test_attention_rows_too_long_to_number(dim, kv_type, heads, tokens):
+    """The first row length behind 2^21 tiles is refused, before any CUDA call (that the last one is taken: test_gpu_kv.py)."""
+    fmt = _fmt(page_tokens=256, n_kv_heads=heads, head_dim=dim, kv_type=kv_type)
+    kw = dict(hq=heads, qs=heads * dim, os=heads * dim)
+    assert _attend(fmt, seqs=_seqs(table_stride=tokens // 256 + 1), **kw) == UNSUPPORTED
+    assert _attend(fmt, seqs=_seqs(table_stride=1 << 22), window=tokens, **kw) == UNSUPPORTED     # (and a tile that it begins inside)
+
+
+def test_attention_too_much_to_number():
+    wide = _fmt(page_tokens=256, n_kv_heads=512, head_dim=128)
+    kw = dict(hq=512, qs=512 * 128, os=512 * 128)
+    assert _attend(wide, seqs=_seqs(table_stride=131072), **kw) == UNSUPPORTED                     # (2^21 + 2) * 512 places of a sequence
+    assert _attend(_fmt(n_pages=1 << 30, page_tokens=8, n_kv_heads=1), hq=1, qs=128, os=128) == UNSUPPORTED    # 2^33 rows of keys
