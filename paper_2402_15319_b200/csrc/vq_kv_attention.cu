@@ -1091,7 +1091,8 @@ vq_status launch(AttnArgs a, const KvGeometry& g, const KvPool& pool, cudaStream
     st = encode_tensor_map(&maps[i], i ? pool.v : pool.k, I8 ? 1 : 2, 2, dims, strides, box, S::CBB == 128 ? 2 : 1);
     if (st != VQ_OK) return st;
   }
-  // as many sequences at a time as have places below 2^30 (tens of terabytes of cache: one launch is what there is)
+  // As many sequences at a time as have places below 2^30, by what their table rows (or the window) have room for: with eight heads
+  // and tiles of 16 tokens, half a million rows of 4096 tokens (more than a call has), 63 of 2^25.
   const long long seqs = 0x3fffffff / per_seq;
   for (long long from = 0, all = a.n_seqs; from < all; from += seqs) {
     a.n_seqs = static_cast<int>(all - from < seqs ? all - from : seqs);

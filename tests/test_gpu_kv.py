@@ -322,6 +322,24 @@ def test_attention_longest_rows(dim, int8, tokens):
         check(c, q, *attend(c, q, 0.1, window, dev=(pool, vq.KVSeqs(table, c.len.to(DEV)))), 0.1, window)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_several_launches(int8):
+    """Wide table rows: a launch numbers the places of so many sequences only, whatever is in the cache.  Sequences of a few
+    tokens, empty ones on both sides of each border, in three launches; rows of outputs and of lse behind the first."""
+    stride, page, heads, dim = 131000, 256, 8, 128
+    at_once = 0x3fffffff // ((stride * page // (32 if int8 else 16) + 2) * heads)
+    n = 2 * at_once + 3
+    lens = _rng_lens(23, n, 0, 300)
+    for border in (at_once, 2 * at_once):
+        lens[border - 1:border + 1] = [0, 5] if border == at_once else [270, 0]
+    c = Cache(lens, heads, dim, page, int8, seed=24, extra_stride=0)
+    pool, _ = c.device()
+    table = torch.full((n, stride), -7, dtype=torch.int32, device=DEV)
+    table[:, :c.table.shape[1]] = c.table.to(DEV)
+    q = queries(n, heads * 2, dim, 25)
+    check(c, q, *attend(c, q, 0.1, dev=(pool, vq.KVSeqs(table, c.len.to(DEV)))), 0.1)
+
+
 # ---- append -------------------------------------------------------------------------------------------------------
 
 def rope_table(n, rot, seed=0):
