@@ -397,8 +397,10 @@ vq_status vq_kv_info(const vq_kv_format* fmt, vq_kv_info_t* out);
  *   d_ws      : at least vq_kv_attention_workspace_bytes(fmt) bytes, 16-byte aligned.  Rules as WORKSPACE above, for
  *               calls of this entry point: zero-filled once, then free for calls of any format, batch and length.
  *               Not to be shared with the products' workspace.
- * Scores, softmax and sums are binary32; one rounding to binary16 at the end.  Masked places and what lies behind a
- * sequence's last token are not read as numbers: an infinity or NaN there changes nothing.
+ * Scores, softmax and sums are binary32; one rounding to binary16 at the end.  A weight (in an 8-bit cache times its
+ * value's scale) meets the values as two binary16 numbers, off by 2^-23 of it or, if that is more, 2^-32 of the largest.
+ * Masked places and what lies behind a sequence's last token are not read as numbers: an infinity or NaN there changes
+ * nothing.
  * Errors: NULL, FORMAT, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED (head_dim; more than a launch can number: table rows, or
  * where there is one windows, of over 2^21 tiles of 16 to 64 tokens - 2^25 tokens are never too many -, or of 2^30 tiles
  * and more, two added each, over all key/value heads and their groups of 8 or 16 query heads; pools of 2^31 rows of

@@ -33,8 +33,9 @@ constexpr int kWaitTries = 1 << 18;     // mbarrier polls before a warp gives up
 constexpr int kMaxHeads = 16;           // query heads that a CTA takes together at most
 constexpr int kMaxCtas = 256;           // CTAs of a launch, one per SM (partial sums and counters are sized for them)
 constexpr int kMaxWarps = 12;
-// Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, weights down to 2^-21 of the largest are normal
-// numbers, and the two binary16 pieces of any weight together are off by 2^-32 of the largest at most.
+// Weights are held as 2^kLift * exp(...): up to 2^(kLift + kSlack) fits binary16, and weights down to 2^-21 of the largest are normal
+// numbers.  The two binary16 pieces of a weight w (w rounded, and the rest rounded) are off by 2^-23 w at most where the second is a
+// normal number, and by 2^-25 where it is not: 2^-32 of the largest weight, which is 2^kLift or more.
 constexpr float kLift = 7.0f, kSlack = 8.0f;
 
 struct AttnArgs {
