@@ -570,6 +570,20 @@ def _here(handles, *tensors) -> None:
             _elsewhere(now, t)
 
 
+_int32 = None
+
+
+def _list(t, n: int) -> None:
+    """A list of the books: contiguous int32, with the n entries that the call reads or writes.  What is missing is the library's to
+    refuse."""
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    if t is not None and (t.dtype is not _int32 or t.numel() < n or not t.is_contiguous()):
+        raise ValueError(f"a contiguous int32 tensor of {n} entries or more is wanted, not {t.dtype} of {tuple(t.shape)}")
+
+
 def _bytes(t) -> int:
     return t.numel() * t.element_size()
 
@@ -597,6 +611,7 @@ def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens
                  rotary: KVRotary | None = None, stream=None) -> None:
     """New tokens into the cache.  d_starts None: one token per sequence."""
     _here((pool, seqs) if rotary is None else (pool, seqs, rotary), d_starts, d_k, d_v)
+    _list(d_starts, seqs._c.n_seqs + 1)
     _room(pool, fmt)
     _check(load().vq_kv_append(fmt._p, pool._p, seqs._p, _ptr(d_starts), n_tokens, _ptr(d_k), k_stride, _ptr(d_v), v_stride,
                                None if rotary is None else rotary._p, _stream(stream)), "vq_kv_append")
@@ -609,6 +624,9 @@ def vq_kv_pages_workspace_bytes(fmt: VQKVFormat, n_seqs: int) -> int:
 def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, stream=None) -> None:
     """Room for d_new tokens per sequence (None: one each); d_status: pages missing, sequences too long."""
     _here((seqs,), d_refs, d_new, d_status, d_ws)
+    _list(d_refs, fmt.n_pages)
+    _list(d_new, seqs._c.n_seqs)
+    _list(d_status, 2)
     _check(load().vq_kv_reserve(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_new), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
                                 _stream(stream)), "vq_kv_reserve")
 
@@ -617,12 +635,17 @@ def vq_kv_fork(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_pairs, n_pairs: i
     """pools: a KVPool per layer (KVPools).  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
     pools = _pools(pools, fmt)
     _here((pools, seqs), d_refs, d_pairs, d_status, d_ws)
+    _list(d_refs, fmt.n_pages)
+    _list(d_pairs, 2 * n_pairs)
+    _list(d_status, 2)
     _check(load().vq_kv_fork(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_pairs), n_pairs, _ptr(d_status),
                              d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
 
 
 def vq_kv_free(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_slots, n_slots: int, stream=None) -> None:
     _here((seqs,), d_refs, d_slots)
+    _list(d_refs, fmt.n_pages)
+    _list(d_slots, n_slots)
     _check(load().vq_kv_free(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_slots), n_slots, _stream(stream)), "vq_kv_free")
 
 
@@ -630,6 +653,8 @@ def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, 
     """d_status: pages in use, pages moved."""
     pools = _pools(pools, fmt)
     _here((pools, seqs), d_refs, d_status, d_ws)
+    _list(d_refs, fmt.n_pages)
+    _list(d_status, 2)
     _check(load().vq_kv_compact(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
                                 _stream(stream)), "vq_kv_compact")
 
@@ -637,6 +662,7 @@ def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, 
 def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None) -> None:
     pools = _pools(pools, fmt)
     _here((pools,), d_pairs)
+    _list(d_pairs, 2 * n_pairs)
     _check(load().vq_kv_copy_pages(fmt._p, pools._p, len(pools.pools), _ptr(d_pairs), n_pairs, _stream(stream)), "vq_kv_copy_pages")
 
 

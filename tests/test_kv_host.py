@@ -282,3 +282,40 @@ def test_attention_too_much_to_number():
     kw = dict(hq=512, qs=512 * 128, os=512 * 128)
     assert _attend(wide, seqs=_seqs(table_stride=131072), **kw) == UNSUPPORTED                     # (2^21 + 2) * 512 places of a sequence
     assert _attend(_fmt(n_pages=1 << 30, page_tokens=8, n_kv_heads=1), hq=1, qs=128, os=128) == UNSUPPORTED    # 2^33 rows of keys
+
+
+def _on_device(monkeypatch):
+    """Host tensors pass as the current device's, and no call gets as far as the library."""
+    monkeypatch.setattr(binding, "_here", lambda *operands: None)
+    monkeypatch.setattr(binding, "load", lambda: pytest.fail("the call went to the library"))
+    monkeypatch.setattr(binding, "_stream", lambda stream: 0)
+
+
+def test_books_check_their_lists(monkeypatch):
+    """Page lists, counts and statuses are contiguous int32 of the lengths that the calls read."""
+    torch = pytest.importorskip("torch")
+    _on_device(monkeypatch)
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    fmt = vq.VQKVFormat(6, 8, 1, 16, vq.VQ_KV_FP16)
+    seqs, ws = vq.KVSeqs(ints(3, 2), ints(3)), torch.zeros(1 << 16, dtype=torch.uint8)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    pools = [vq.KVPool(half(6, 1, 8, 16), half(6, 1, 8, 16))]
+    good = dict(refs=ints(6), new=ints(3), status=ints(2), pairs=ints(4, 2), slots=ints(4), starts=ints(4))
+    calls = {
+        "reserve": (lambda a: vq.vq_kv_reserve(fmt, seqs, a["refs"], a["new"], a["status"], ws), ("refs", "new", "status")),
+        "fork": (lambda a: vq.vq_kv_fork(fmt, pools, seqs, a["refs"], a["pairs"], 4, a["status"], ws), ("refs", "pairs", "status")),
+        "free": (lambda a: vq.vq_kv_free(fmt, seqs, a["refs"], a["slots"], 4), ("refs", "slots")),
+        "compact": (lambda a: vq.vq_kv_compact(fmt, pools, seqs, a["refs"], a["status"], ws), ("refs", "status")),
+        "copy_pages": (lambda a: vq.vq_kv_copy_pages(fmt, pools, a["pairs"], 4), ("pairs",)),
+        "append": (lambda a: vq.vq_kv_append(fmt, pools[0], seqs, a["starts"], 5, half(5, 16), 16, half(5, 16), 16), ("starts",)),
+    }
+    for name, (call, used) in calls.items():
+        for key in used:
+            t = good[key]
+            for bad in (t.long(), t.float(), torch.zeros(2 * t.numel(), dtype=torch.int32)[::2], t.reshape(-1)[:-1].clone(), t.reshape(-1)[:0]):
+                with pytest.raises(ValueError, match="int32"):
+                    call({**good, key: bad})
+        with pytest.raises(pytest.fail.Exception, match="library"):       # the good ones go through
+            call(good)
+    with pytest.raises(pytest.fail.Exception, match="library"):           # one token each: no counts
+        calls["reserve"][0]({**good, "new": None})
