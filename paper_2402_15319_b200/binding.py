@@ -487,6 +487,7 @@ class KVRotary(_Held):
         t = self.d_cos_sin
         if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < self.n_positions * self.rot_dim):
             raise ValueError("KVRotary: contiguous float32 cosines and sines, rot_dim of them for every position")
+        _halves(self.d_q, self.d_q_out)
         self._hold(_CKVRotary(_ptr(self.d_cos_sin), int(self.n_positions), int(self.rot_dim), int(self.interleaved), int(self.n_q_heads),
                               _ptr(self.d_q), _ptr(self.d_q_out), int(self.q_stride), int(self.q_out_stride)),
                    _device_of(self.d_cos_sin, self.d_q, self.d_q_out))
@@ -570,16 +571,36 @@ def _here(handles, *tensors) -> None:
             _elsewhere(now, t)
 
 
-_int32 = None
+_int32 = _float16 = _float32 = None
+
+
+def _types() -> None:
+    global _int32, _float16, _float32
+    import torch
+    _int32, _float16, _float32 = torch.int32, torch.float16, torch.float32
+
+
+def _halves(*operands) -> None:
+    if _float16 is None:
+        _types()
+    for t in operands:
+        if t is not None and t.dtype is not _float16:
+            raise ValueError(f"a float16 tensor is wanted, not {t.dtype}")
+
+
+def _singles(*operands) -> None:
+    if _float32 is None:
+        _types()
+    for t in operands:
+        if t is not None and t.dtype is not _float32:
+            raise ValueError(f"a float32 tensor is wanted, not {t.dtype}")
 
 
 def _list(t, n: int) -> None:
     """A list of the books: contiguous int32, with the n entries that the call reads or writes.  What is missing is the library's to
     refuse."""
-    global _int32
     if _int32 is None:
-        import torch
-        _int32 = torch.int32
+        _types()
     if t is not None and (t.dtype is not _int32 or t.numel() < n or not t.is_contiguous()):
         raise ValueError(f"a contiguous int32 tensor of {n} entries or more is wanted, not {t.dtype} of {tuple(t.shape)}")
 
@@ -602,6 +623,9 @@ def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int,
                     window: int, d_ws, stream=None) -> None:
     """One new token per sequence over the paged cache; window 0: all of it.  d_lse may be None."""
     _here((pool, seqs), d_q, d_out, d_lse, d_ws)
+    _halves(d_q, d_out)
+    if d_lse is not None:
+        _singles(d_lse)
     _room(pool, fmt)
     _check(load().vq_kv_attention(fmt._p, pool._p, seqs._p, n_q_heads, _ptr(d_q), q_stride, _ptr(d_out), out_stride, _ptr(d_lse), scale,
                                   window, d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_attention")
@@ -612,6 +636,7 @@ def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens
     """New tokens into the cache.  d_starts None: one token per sequence."""
     _here((pool, seqs) if rotary is None else (pool, seqs, rotary), d_starts, d_k, d_v)
     _list(d_starts, seqs._c.n_seqs + 1)
+    _halves(d_k, d_v)
     _room(pool, fmt)
     _check(load().vq_kv_append(fmt._p, pool._p, seqs._p, _ptr(d_starts), n_tokens, _ptr(d_k), k_stride, _ptr(d_v), v_stride,
                                None if rotary is None else rotary._p, _stream(stream)), "vq_kv_append")
@@ -669,5 +694,7 @@ def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None)
 def vq_residual_norm(norm: VQNorm, d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h, stream=None) -> None:
     """x' = x + residual_scale * gate * post(y), h = pre(x'); absent operands are None."""
     _here((), d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h)
+    _halves(d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_h)
+    (_singles if norm.residual_type == VQ_RESIDUAL_FP32 else _halves)(d_x, d_x_out)
     _check(load().vq_residual_norm(norm._p, _ptr(d_x), _ptr(d_y), _ptr(d_gate), _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b),
                                    _ptr(d_x_out), _ptr(d_h), _stream(stream)), "vq_residual_norm")

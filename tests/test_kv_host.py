@@ -319,3 +319,35 @@ def test_books_check_their_lists(monkeypatch):
             call(good)
     with pytest.raises(pytest.fail.Exception, match="library"):           # one token each: no counts
         calls["reserve"][0]({**good, "new": None})
+
+
+def test_operands_of_another_type_are_refused(monkeypatch):
+    """bfloat16 has binary16's size: read as it, it would give numbers, and wrong ones."""
+    torch = pytest.importorskip("torch")
+    _on_device(monkeypatch)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    f32 = lambda *s: torch.zeros(s, dtype=torch.float32)  # noqa: E731
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    fmt = vq.VQKVFormat(6, 8, 1, 64, vq.VQ_KV_FP16)
+    pool, seqs, ws = vq.KVPool(half(6, 1, 8, 64), half(6, 1, 8, 64)), vq.KVSeqs(ints(3, 2), ints(3)), torch.zeros(1 << 16, dtype=torch.uint8)
+    norm = vq.VQNorm(4, 64, vq.VQ_NORM_LAYER, vq.VQ_RESIDUAL_FP16, vq.VQ_GATE_ELEMENT, 1e-5, 1.0, 64, 64, 64, 64, 64)
+    wide = vq.VQNorm(**{**norm.__dict__, "residual_type": vq.VQ_RESIDUAL_FP32})
+    rows, line = half(4, 64), half(64)
+    calls = [
+        (lambda q, out, lse: vq.vq_kv_attention(fmt, pool, seqs, 1, q, 64, out, 64, lse, 0.1, 0, ws), (half(3, 64), half(3, 64), f32(3, 1))),
+        (lambda k, v: vq.vq_kv_append(fmt, pool, seqs, None, 3, k, 64, v, 64), (half(3, 64), half(3, 64))),
+        (lambda *t: vq.vq_residual_norm(norm, *t), (rows, rows, rows, line, line, line, line, rows, rows)),
+        (lambda *t: vq.vq_residual_norm(wide, *t), (f32(4, 64), rows, rows, line, line, line, line, f32(4, 64), rows)),
+    ]
+    for call, good in calls:
+        for i, t in enumerate(good):
+            for other in (torch.bfloat16, torch.float32 if t.dtype == torch.float16 else torch.float16, torch.int16):
+                with pytest.raises(ValueError, match="float"):
+                    call(*good[:i], t.to(other), *good[i + 1:])
+        with pytest.raises(pytest.fail.Exception, match="library"):
+            call(*good)
+    with pytest.raises(pytest.fail.Exception, match="library"):           # absent operands
+        vq.vq_residual_norm(norm, rows, None, None, None, None, line, None, None, rows)
+    for q, out in ((rows.bfloat16(), rows), (rows, f32(4, 64))):
+        with pytest.raises(ValueError, match="float"):
+            vq.KVRotary(f32(16, 32, 2), 16, 64, 0, 1, q, 64, out, 64)
