@@ -491,6 +491,48 @@ def test_append_int8_nearest_integers(dim, heads, tokens):
         assert np.array_equal(scale[where, :, slot].numpy(), x.float().abs().amax(-1).numpy() / np.float32(127))
 
 
+@pytest.mark.parametrize("dim", [192, 256])
+@pytest.mark.parametrize("int8", [False, True])
+def test_append_in_place_heads_spread(dim, int8):
+    """Few tokens, wide heads: a token's heads are shared by several CTAs, each turning its queries where they lie."""
+    c = Cache([5, 33, 1], 4, dim, 16, int8, seed=dim, extra_stride=0)
+    check_append(c, None, rows(3, 4, dim, 41), rows(3, 4, dim, 42), rows(3, 32, dim, 43), rope_table(c.table.shape[1] * 16, dim), dim, 1, in_place=True)
+
+
+def test_append_and_pages_on_two_streams():
+    """Two caches, a stream each, at the same time: as one after the other."""
+    dev = [DeviceBooks(kv_ref.Books(400, 8, 40, 12), 1, 1, 64, False, seed=s) for s in (51, 52)]
+    streams = [torch.cuda.Stream(DEV) for _ in dev]
+    n = 40
+    k, v = rows(n, 1, 64, 53).reshape(n, 64).to(DEV), rows(n, 1, 64, 54).reshape(n, 64).to(DEV)
+    cs = rope_table(12 * 8, 64).to(DEV)
+    leave, pairs = dev[0].ints([3, 4, 5]), dev[0].ints([[0, 3], [1, 4]])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for d, st in zip(dev, streams):
+            vq.vq_kv_reserve(d.fmt, d.seqs, d.refs, None, d.status, d.ws, stream=st)
+            vq.vq_kv_append(d.fmt, d.pools[0], d.seqs, None, n, k, 64, v, 64, vq.KVRotary(cs, 96, 64, 0), stream=st)
+    for d, st in zip(dev, streams):
+        vq.vq_kv_free(d.fmt, d.seqs, d.refs, leave, 3, stream=st)
+        vq.vq_kv_fork(d.fmt, d.pools, d.seqs, d.refs, pairs, 2, d.status, d.ws, stream=st)
+        vq.vq_kv_compact(d.fmt, d.pools, d.seqs, d.refs, d.status, d.ws, stream=st)
+    torch.cuda.synchronize()
+    for d in dev:
+        for _ in range(20):
+            assert d.m.reserve([1] * n) == (0, 0)
+        d.m.free([3, 4, 5])
+        d.m.fork([(0, 3), (1, 4)])
+        assert tuple(d.status.cpu().tolist()) == d.m.compact()[0]
+        assert d.table.cpu().tolist() == d.m.table and d.len.cpu().tolist() == d.m.len and d.refs.cpu().tolist() == d.m.refs
+        pool_k, pool_v = d.pools[0].k.cpu(), d.pools[0].v.cpu()
+        for s in (0, 3, 4, 39):
+            at = torch.arange(20)
+            where, slot = torch.tensor(d.m.table[s])[at // 8].long(), at % 8
+            of = {3: 0, 4: 1}.get(s, s)     # the forked ones hold their parents' tokens
+            assert torch.equal(pool_v[where, 0, slot], v[of].cpu().expand(20, 64))
+            assert torch.equal(pool_k[where, 0, slot][0], k[of].cpu())     # (position 0: cosine 1, sine 0)
+
+
 # ---- pages ----------------------------------------------------------------------------------------------------------
 
 class DeviceBooks:
@@ -713,6 +755,34 @@ def test_norm(n_rows, n_cols, layer, post, gate, wide):
     got = h[:, :n_cols].cpu().double()
     tol = HALF * ref.abs() + SUB + 2 * sh
     assert bool(((got - ref).abs() <= tol).all()), float(((got - ref).abs() / tol).max())
+
+
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("n_rows,n_cols", [(5, 96), (5, 5000), (400, 4096), (400, 600), (320, 1001)])
+def test_norm_rows_that_overflow(n_rows, n_cols, layer):
+    """An infinity or NaN stays in its row; a sum beyond binary16 is stored as an infinity, and its row is normed before that."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n_cols)
+    x, y = (torch.randn(n_rows, n_cols, generator=g, device=DEV).half() for _ in range(2))
+    w = torch.randn(n_cols, generator=g, device=DEV).half()
+    nb = vq.VQNorm(n_rows, n_cols, int(layer), vq.VQ_RESIDUAL_FP16, vq.VQ_GATE_NONE, 1e-5, 1.0, n_cols, n_cols, 0, n_cols, n_cols)
+    out, h, out2, h2 = (torch.empty_like(x) for _ in range(4))
+    vq.vq_residual_norm(nb, x, y, None, None, None, w, None, out, h)
+    x2, y2 = x.clone(), y.clone()
+    x2[1, 7], y2[2, n_cols - 1] = float("inf"), float("nan")
+    x2[3, 5] = y2[3, 5] = 60000.0
+    vq.vq_residual_norm(nb, x2, y2, None, None, None, w, None, out2, h2)
+    torch.cuda.synchronize()
+    same = torch.ones(n_rows, dtype=torch.bool, device=DEV)
+    same[1:4] = False
+    assert torch.equal(out[same], out2[same]) and torch.equal(h[same], h2[same])
+    want = (x2.float() + y2.float()).half()
+    assert torch.equal(out2[[1, 3]], want[[1, 3]]) and bool(torch.isinf(out2[3, 5])) and bool(torch.isnan(out2[2, n_cols - 1]))
+    assert bool(torch.isnan(h2[2]).all()) and bool(torch.isnan(h2[1, 7]))
+    ref, slop = norm_ref((x2[3:4].cpu().double() + y2[3:4].cpu().double()), layer, w.cpu().double(), None, float(np.float32(1e-5)))
+    got = h2[3:4].cpu().double()
+    slop = 2 * slop + 4 * 2.0 ** -24 * ref.abs()
+    assert bool(((got - ref).abs() <= HALF * ref.abs() + SUB + slop).all())
 
 
 @pytest.mark.parametrize("n_cols", [96, 5000])
