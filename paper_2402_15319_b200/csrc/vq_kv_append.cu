@@ -6,7 +6,7 @@
 // so the token's cosines and sines are fetched once per thread and used for all of them.  A group of LG lanes holds a head's row:
 // a lane two 16-byte pieces, the two halves of the pairs that it turns, so that nothing crosses lanes but the 8-bit
 // row's maximum.
-// 8192 tokens, 64/8 heads of 128: 57 us into 8-bit pages, 58 into binary16 ones = 5.8 TB/s; a token each of 16 sequences: 1.8 us.
+// 8192 tokens, 64/8 heads of 128: 57.5 us into 8-bit pages, 58 into binary16 ones = 5.8 TB/s; a token each of 16 sequences: 2.0 us.
 #include "vq_device.cuh"
 #include "vq_kv.cuh"
 

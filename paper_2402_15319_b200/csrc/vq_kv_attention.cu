@@ -139,7 +139,9 @@ struct Shape {
   static constexpr int NS = fit(WARPS) > 6 ? 6 : fit(WARPS);   // stages of a warp's ring
   static constexpr int RINGS = WARPS * NS * STAGE;
   static constexpr size_t SMEM = 1024 + static_cast<size_t>(RINGS) + WARPS * NS * SCALES;   // (1024: alignment)
-  // Costs of a split (see choose()): measured from calls of 1 to 16 sequences, 8 to 128 heads, 100 to 4096 tokens.
+  // Costs of a split (see choose()): measured from calls of 1 to 16 sequences, 8 to 128 heads, 100 to 4096 tokens, up to 8 query heads to
+  // a key/value head; elsewhere they are carried over.  A join costs more the more CTAs share a head, which no term counts: one
+  // sequence of 32768 tokens with one key/value head takes 44 us with 8 query heads of 128, 157 with 16 of 256.
   static constexpr float JOIN_COST = 22.0f * 8192 / STAGE, RUN_COST = 31.0f * 8192 / STAGE, ALONE = I8 ? 1.11f : 0.625f;
   static constexpr int QREGS = D / 16 * 2 * NH;
   static constexpr bool AHEAD = QREGS <= 32;            // the next piece's queries are fetched under this one

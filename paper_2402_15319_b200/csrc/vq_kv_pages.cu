@@ -5,7 +5,8 @@
 // 65,536 pages took 8.5 us), ballots make words of them that go to the first CTA's shared memory, and scans of the words'
 // counts rank the pages, so equal books give equal books.  What does not depend on order - page data, table rows, counts
 // of shared pages - is left to a second kernel on the whole GPU, which finds the list of pages in the workspace.
-// Counting 65,536 pages and entering 1750 for 256 sequences: 7.8 us; moving 980 pages of 32 KB in 8 layers: 174 us = 5.9 TB/s.
+// Counting 65,536 pages and entering 1750 for 256 sequences: 8.3 us with a copy of the books in front (alone 1.6); moving
+// 980 pages of 32 KB in 8 layers: 174 us = 5.9 TB/s.
 #include "vq_device.cuh"
 #include "vq_kv.cuh"
 
