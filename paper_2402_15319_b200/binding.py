@@ -487,7 +487,9 @@ class KVRotary(_Held):
         t = self.d_cos_sin
         if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < self.n_positions * self.rot_dim):
             raise ValueError("KVRotary: contiguous float32 cosines and sines, rot_dim of them for every position")
-        _halves(self.d_q, self.d_q_out)
+        for t in (self.d_q, self.d_q_out):
+            if t is not None and t.dtype != torch.float16:
+                raise ValueError("KVRotary: float16 queries")
         self._hold(_CKVRotary(_ptr(self.d_cos_sin), int(self.n_positions), int(self.rot_dim), int(self.interleaved), int(self.n_q_heads),
                               _ptr(self.d_q), _ptr(self.d_q_out), int(self.q_stride), int(self.q_out_stride)),
                    _device_of(self.d_cos_sin, self.d_q, self.d_q_out))
@@ -560,8 +562,13 @@ def _elsewhere(now, *operands):
                 raise ValueError(f"operand on device {dev}, the current device is cuda:{now}")
 
 
-def _here(handles, *tensors) -> None:
-    """The calls below launch on the current device: operands of another one (or of the host) are refused."""
+_int32 = _float16 = _float32 = None
+
+
+def _here(handles, *tensors) -> int:
+    """The calls below launch on the current device, which is returned: operands of another one (or of the host) are refused."""
+    if _int32 is None:
+        _types()
     now = _device_now()
     for h in handles:
         if h.device != now:
@@ -569,9 +576,7 @@ def _here(handles, *tensors) -> None:
     for t in tensors:
         if t is not None and t.get_device() != now:
             _elsewhere(now, t)
-
-
-_int32 = _float16 = _float32 = None
+    return now
 
 
 def _types() -> None:
@@ -580,28 +585,18 @@ def _types() -> None:
     _int32, _float16, _float32 = torch.int32, torch.float16, torch.float32
 
 
-def _halves(*operands) -> None:
-    if _float16 is None:
-        _types()
+def _of_type(now, dtype, *operands) -> None:
     for t in operands:
-        if t is not None and t.dtype is not _float16:
-            raise ValueError(f"a float16 tensor is wanted, not {t.dtype}")
+        if t is not None and (t.dtype is not dtype or t.get_device() != now):
+            _elsewhere(now, t)
+            raise ValueError(f"a {dtype} tensor is wanted, not {t.dtype}")
 
 
-def _singles(*operands) -> None:
-    if _float32 is None:
-        _types()
-    for t in operands:
-        if t is not None and t.dtype is not _float32:
-            raise ValueError(f"a float32 tensor is wanted, not {t.dtype}")
-
-
-def _list(t, n: int) -> None:
+def _list(now, t, n: int) -> None:
     """A list of the books: contiguous int32, with the n entries that the call reads or writes.  What is missing is the library's to
     refuse."""
-    if _int32 is None:
-        _types()
-    if t is not None and (t.dtype is not _int32 or t.numel() < n or not t.is_contiguous()):
+    if t is not None and (t.dtype is not _int32 or t.get_device() != now or t.numel() < n or not t.is_contiguous()):
+        _elsewhere(now, t)
         raise ValueError(f"a contiguous int32 tensor of {n} entries or more is wanted, not {t.dtype} of {tuple(t.shape)}")
 
 
@@ -622,10 +617,9 @@ def vq_kv_attention_workspace_bytes(fmt: VQKVFormat) -> int:
 def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int, d_q, q_stride: int, d_out, out_stride: int, d_lse, scale: float,
                     window: int, d_ws, stream=None) -> None:
     """One new token per sequence over the paged cache; window 0: all of it.  d_lse may be None."""
-    _here((pool, seqs), d_q, d_out, d_lse, d_ws)
-    _halves(d_q, d_out)
-    if d_lse is not None:
-        _singles(d_lse)
+    now = _here((pool, seqs), d_ws)
+    _of_type(now, _float16, d_q, d_out)
+    _of_type(now, _float32, d_lse)
     _room(pool, fmt)
     _check(load().vq_kv_attention(fmt._p, pool._p, seqs._p, n_q_heads, _ptr(d_q), q_stride, _ptr(d_out), out_stride, _ptr(d_lse), scale,
                                   window, d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_attention")
@@ -634,9 +628,9 @@ def vq_kv_attention(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, n_q_heads: int,
 def vq_kv_append(fmt: VQKVFormat, pool: KVPool, seqs: KVSeqs, d_starts, n_tokens: int, d_k, k_stride: int, d_v, v_stride: int,
                  rotary: KVRotary | None = None, stream=None) -> None:
     """New tokens into the cache.  d_starts None: one token per sequence."""
-    _here((pool, seqs) if rotary is None else (pool, seqs, rotary), d_starts, d_k, d_v)
-    _list(d_starts, seqs._c.n_seqs + 1)
-    _halves(d_k, d_v)
+    now = _here((pool, seqs) if rotary is None else (pool, seqs, rotary))
+    _list(now, d_starts, seqs._c.n_seqs + 1)
+    _of_type(now, _float16, d_k, d_v)
     _room(pool, fmt)
     _check(load().vq_kv_append(fmt._p, pool._p, seqs._p, _ptr(d_starts), n_tokens, _ptr(d_k), k_stride, _ptr(d_v), v_stride,
                                None if rotary is None else rotary._p, _stream(stream)), "vq_kv_append")
@@ -648,10 +642,10 @@ def vq_kv_pages_workspace_bytes(fmt: VQKVFormat, n_seqs: int) -> int:
 
 def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, stream=None) -> None:
     """Room for d_new tokens per sequence (None: one each); d_status: pages missing, sequences too long."""
-    _here((seqs,), d_refs, d_new, d_status, d_ws)
-    _list(d_refs, fmt.n_pages)
-    _list(d_new, seqs._c.n_seqs)
-    _list(d_status, 2)
+    now = _here((seqs,), d_ws)
+    _list(now, d_refs, fmt.n_pages)
+    _list(now, d_new, seqs._c.n_seqs)
+    _list(now, d_status, 2)
     _check(load().vq_kv_reserve(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_new), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
                                 _stream(stream)), "vq_kv_reserve")
 
@@ -659,42 +653,41 @@ def vq_kv_reserve(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_new, d_status, d_ws, 
 def vq_kv_fork(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_pairs, n_pairs: int, d_status, d_ws, stream=None) -> None:
     """pools: a KVPool per layer (KVPools).  d_pairs: (parent, child) rows; d_status: pages missing, entries left out."""
     pools = _pools(pools, fmt)
-    _here((pools, seqs), d_refs, d_pairs, d_status, d_ws)
-    _list(d_refs, fmt.n_pages)
-    _list(d_pairs, 2 * n_pairs)
-    _list(d_status, 2)
+    now = _here((pools, seqs), d_ws)
+    _list(now, d_refs, fmt.n_pages)
+    _list(now, d_pairs, 2 * n_pairs)
+    _list(now, d_status, 2)
     _check(load().vq_kv_fork(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_pairs), n_pairs, _ptr(d_status),
                              d_ws.data_ptr(), _bytes(d_ws), _stream(stream)), "vq_kv_fork")
 
 
 def vq_kv_free(fmt: VQKVFormat, seqs: KVSeqs, d_refs, d_slots, n_slots: int, stream=None) -> None:
-    _here((seqs,), d_refs, d_slots)
-    _list(d_refs, fmt.n_pages)
-    _list(d_slots, n_slots)
+    now = _here((seqs,))
+    _list(now, d_refs, fmt.n_pages)
+    _list(now, d_slots, n_slots)
     _check(load().vq_kv_free(fmt._p, seqs._p, _ptr(d_refs), _ptr(d_slots), n_slots, _stream(stream)), "vq_kv_free")
 
 
 def vq_kv_compact(fmt: VQKVFormat, pools, seqs: KVSeqs, d_refs, d_status, d_ws, stream=None) -> None:
     """d_status: pages in use, pages moved."""
     pools = _pools(pools, fmt)
-    _here((pools, seqs), d_refs, d_status, d_ws)
-    _list(d_refs, fmt.n_pages)
-    _list(d_status, 2)
+    now = _here((pools, seqs), d_ws)
+    _list(now, d_refs, fmt.n_pages)
+    _list(now, d_status, 2)
     _check(load().vq_kv_compact(fmt._p, pools._p, len(pools.pools), seqs._p, _ptr(d_refs), _ptr(d_status), d_ws.data_ptr(), _bytes(d_ws),
                                 _stream(stream)), "vq_kv_compact")
 
 
 def vq_kv_copy_pages(fmt: VQKVFormat, pools, d_pairs, n_pairs: int, stream=None) -> None:
     pools = _pools(pools, fmt)
-    _here((pools,), d_pairs)
-    _list(d_pairs, 2 * n_pairs)
+    _list(_here((pools,)), d_pairs, 2 * n_pairs)
     _check(load().vq_kv_copy_pages(fmt._p, pools._p, len(pools.pools), _ptr(d_pairs), n_pairs, _stream(stream)), "vq_kv_copy_pages")
 
 
 def vq_residual_norm(norm: VQNorm, d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h, stream=None) -> None:
     """x' = x + residual_scale * gate * post(y), h = pre(x'); absent operands are None."""
-    _here((), d_x, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_x_out, d_h)
-    _halves(d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_h)
-    (_singles if norm.residual_type == VQ_RESIDUAL_FP32 else _halves)(d_x, d_x_out)
+    now = _here(())
+    _of_type(now, _float16, d_y, d_gate, d_post_w, d_post_b, d_pre_w, d_pre_b, d_h)
+    _of_type(now, _float32 if norm.residual_type == VQ_RESIDUAL_FP32 else _float16, d_x, d_x_out)
     _check(load().vq_residual_norm(norm._p, _ptr(d_x), _ptr(d_y), _ptr(d_gate), _ptr(d_post_w), _ptr(d_post_b), _ptr(d_pre_w), _ptr(d_pre_b),
                                    _ptr(d_x_out), _ptr(d_h), _stream(stream)), "vq_residual_norm")
