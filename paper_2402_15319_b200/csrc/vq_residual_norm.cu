@@ -353,7 +353,7 @@ vq_status launch_rows(const ResidualNorm& a, int sms, cudaStream_t s) {
 
 template <bool VEC, bool WIDE, bool WARP_ROW, int PER, int MAX_THREADS>
 vq_status launch_one(const ResidualNorm& a, int threads, bool many, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(WARP_ROW ? (a.rows + threads / 32 - 1) / (threads / 32) : a.rows)), block(static_cast<unsigned>(threads));
+  const dim3 grid(static_cast<unsigned>(WARP_ROW ? (a.rows - 1) / (threads / 32) + 1 : a.rows)), block(static_cast<unsigned>(threads));
   if (!many) return launch_dependent(residual_norm_kernel<VEC, WIDE, WARP_ROW, PER, MAX_THREADS, false>, grid, block, 0, s, a);
   residual_norm_kernel<VEC, WIDE, WARP_ROW, PER, MAX_THREADS, true><<<grid, block, 0, s>>>(a);
   return check_launch();

@@ -827,6 +827,16 @@ def test_norm_in_place_many_rows(n_rows, n_cols, wide):
     assert torch.equal(x, out) and torch.equal(y, h)
 
 
+def test_norm_most_rows():
+    """2^31 - 1 rows, the most that a block can name: counts of warps and CTAs rounded up stay in range."""
+    n = 2 ** 31 - 1
+    x = torch.arange(1 << 16, device=DEV).to(torch.int16).repeat(1 << 15)[:n].view(torch.float16)     # every pattern of 16 bits, again and again
+    out = torch.zeros(n, dtype=torch.float16, device=DEV)
+    vq.vq_residual_norm(vq.VQNorm(n, 1, vq.VQ_NORM_RMS, vq.VQ_RESIDUAL_FP16, vq.VQ_GATE_NONE, 1e-5, 1.0, 1, 0, 0, 1, 0), x, None, None, None, None, None, None,
+                        out, None)
+    assert bool(((out.view(torch.int16) == x.view(torch.int16)) | (torch.isnan(out) & torch.isnan(x))).all())
+
+
 # ---- a decode step ---------------------------------------------------------------------------------------------------------
 
 def test_decode_steps_of_a_block():
